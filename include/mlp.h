@@ -327,6 +327,107 @@ mlp_status mlp_deep_last_kernel_ms(mlp_deep_t ctx, float *ms);
 /* Release the host-side context. */
 void mlp_deep_destroy(mlp_deep_t ctx);
 
+/* ---- Layers: a dense layer and dropout ------------------------------------------
+ * The pieces of a net of the caller's own shape, next to the whole nets above: any
+ * widths, a bias, other activations, residuals, dropout, three types, forward and
+ * backward. Row-major matrices whose rows lie ld elements apart (ld >= the number of
+ * columns; elements of a row are adjacent), aligned to their element; what lies between
+ * the rows is neither used nor written. Sums and the arithmetic between a call's reads
+ * and writes are fp32 (the products of fp32 operands as in the first section, with its
+ * two limits of the split); results are rounded once to the call's type, but for the
+ * gradient g of mlp_linear_backward. Results are bitwise reproducible. Conventions
+ * (device pointers, asynchronous stream semantics, host-side argument checks before
+ * anything is enqueued, capture into HIP graphs) are those of the calls above. */
+typedef enum { MLP_F32 = 0, MLP_BF16 = 1, MLP_F16 = 2 } mlp_dtype;
+
+/* a(z): z; max(z, 0) (a NaN passes, a'(0) = 0); z Phi(z), Phi the normal distribution
+ * function; z / (1 + exp(-2 sqrt(2 / pi) (z + 0.044715 z^3))); z / (1 + exp(-z)). */
+typedef enum {
+    MLP_ACT_NONE = 0,
+    MLP_ACT_RELU = 1,
+    MLP_ACT_GELU = 2,
+    MLP_ACT_GELU_TANH = 3,
+    MLP_ACT_SILU = 4
+} mlp_activation;
+
+/* Dropout, in every call below that takes (p, rng). Element (r, c) of a [rows x cols]
+ * matrix is kept where its 16 random bits are at least T = round(p 2^16); what is kept
+ * is divided by q = 1 - T 2^-16, what is dropped becomes 0 whatever it was (p is thus
+ * taken to the nearest multiple of 2^-16, and the expected value is exact for it). The
+ * bits are part c % 8 (the low half of word 0 first) of the Philox4x32-10 block (Salmon,
+ * Moraes, Dror and Shaw, SC'11) with the key rng[0] and the counter
+ * rng[1] + r ceil(cols / 8) + c / 8 (mod 2^64). The mask is never stored: the backward
+ * call recomputes it from the same rng, rows and cols. A call uses rows ceil(cols / 8)
+ * counters; calls whose counter ranges do not meet draw independent masks.
+ *   p    0 <= p <= 1; 0 (as taken): no dropout, rng may be NULL
+ *   rng  device uint64 [2]: seed, offset; read when the work runs (so a replayed graph
+ *        draws new masks when the caller advances it), never written */
+
+/* Bytes of device workspace a dense layer's context needs; 0 for an unsupported shape:
+ * d_in and d_out in [1, 2^20], max_rows in [1, MLP_MAX_BATCH], dtype an mlp_dtype. */
+size_t mlp_linear_workspace_bytes(int32_t dtype, int64_t d_in, int64_t d_out, int64_t max_rows);
+
+/* Create a dense layer's context bound to caller-owned parameters and workspace, on the
+ * current device.
+ *   dtype       type of every matrix of the calls
+ *   activation  an mlp_activation
+ *   max_rows    most rows later calls will use
+ *   W           [d_in x d_out] contiguous, rows = inputs; read by every call
+ *   bias        nullable [d_out]
+ *   workspace   device buffer of at least mlp_linear_workspace_bytes bytes, 256-byte
+ *               aligned, kept alive for the life of the context
+ *   stream      hipStream_t of that device to enqueue on (NULL = the null stream)
+ * Nothing is enqueued. *out is set only on success. Calls on one context must not
+ * overlap, nor replays of graphs that hold calls on it (they share the workspace). */
+typedef struct mlp_linear_ctx *mlp_linear_t;
+mlp_status mlp_linear_init(mlp_linear_t *out, int32_t dtype, int64_t d_in, int64_t d_out,
+                           int32_t activation, int64_t max_rows, const void *W, const void *bias,
+                           void *workspace, size_t ws_bytes, void *stream);
+
+/* Rebind the stream later calls enqueue on (of the context's device). */
+mlp_status mlp_linear_set_stream(mlp_linear_t ctx, void *stream);
+
+/* z = X W + bias;  Y = residual + dropout(a(z)).
+ *   X         [rows x d_in], 0 <= rows <= max_rows (0: nothing is done)
+ *   residual  nullable [rows x d_out]; may be Y itself (same pointer and stride)
+ *   Y         [rows x d_out]
+ *   Z         nullable [rows x d_out]: receives z, which mlp_linear_backward takes
+ * Y and Z must not overlap each other's elements, X, W or bias. */
+mlp_status mlp_linear_forward(mlp_linear_t ctx, const void *X, int64_t ldx, int64_t rows,
+                              const void *residual, int64_t ldr, float p, const uint64_t *rng,
+                              void *Y, int64_t ldy, void *Z, int64_t ldz);
+
+/* Gradients for dY = the loss's gradient in Y (which is also the residual's):
+ *   g = dropout(dY) a'(Z);  dX = g W^T;  dW = X^T g;  dbias = column sums of g.
+ * g is rounded to the call's type for the two products where that is bf16 or fp16 (the
+ * matrix cores take such operands); dbias is summed from the unrounded g.
+ *   X      [rows x d_in] as in the forward call (used by dW only; may be NULL without)
+ *   Z      [rows x d_out] from the forward call; NULL only if the activation is NONE
+ *   dY     [rows x d_out];  p, rng as in the forward call
+ *   dX     nullable [rows x d_in];  dW nullable [d_in x d_out] contiguous;
+ *   dbias  nullable [d_out]; those given are overwritten, also when rows is 0
+ * No output may overlap an input or another output. */
+mlp_status mlp_linear_backward(mlp_linear_t ctx, const void *X, int64_t ldx, const void *Z,
+                               int64_t ldz, const void *dY, int64_t lddy, int64_t rows, float p,
+                               const uint64_t *rng, void *dX, int64_t lddx, void *dW, void *dbias);
+
+/* Release the host-side context. */
+void mlp_linear_destroy(mlp_linear_t ctx);
+
+/* Y = residual + dropout(X): rows and cols >= 0 (0: nothing is done), rows * cols and
+ * rows * each stride below 2^46; residual nullable; Y may be X or residual itself (same
+ * pointer and stride) and must not overlap them otherwise. stream belongs to the
+ * current device. */
+mlp_status mlp_dropout_forward(int32_t dtype, int64_t rows, int64_t cols, const void *X, int64_t ldx,
+                               const void *residual, int64_t ldr, float p, const uint64_t *rng,
+                               void *Y, int64_t ldy, void *stream);
+
+/* dX = dropout(dY), the gradient of mlp_dropout_forward with the same p, rng, rows and
+ * cols (the residual's gradient is dY); dX may be dY itself. */
+mlp_status mlp_dropout_backward(int32_t dtype, int64_t rows, int64_t cols, const void *dY,
+                                int64_t lddy, float p, const uint64_t *rng, void *dX, int64_t lddx,
+                                void *stream);
+
 /* Static description of a status code: any int32 value (a code that is not an
  * mlp_status gives "unknown status"). */
 const char *mlp_status_string(int32_t status);

@@ -1,0 +1,162 @@
+// layer.h -- what the layer operators (linear.hip, dropout.hip) share: element types,
+// activations and their derivatives, and dropout from the Philox4x32-10 counter-based
+// generator (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random numbers: as easy
+// as 1, 2, 3", SC'11).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "bf16x3.h"
+#include "mlp.h"
+
+namespace mlp {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// Eight consecutive elements of a row, as a lane holds them between memory and fp32
+// registers. Rows are aligned to their element only: the packed words let the compiler
+// use the widest load there is at any address.
+template <class T>
+struct __attribute__((packed, aligned(sizeof(T)))) Oct {
+    T e[8];
+};
+
+__device__ __forceinline__ float up(float v) { return v; }
+__device__ __forceinline__ float up(bf16 v) { return (float)v; }
+__device__ __forceinline__ float up(f16 v) { return (float)v; }
+
+// columns [c, c + 8) of the row at p into v; columns from n on read nothing and give 0
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int64_t c, int64_t n, float (&v)[8]) {
+    if (c + 8 <= n) {
+        const Oct<T> o = *reinterpret_cast<const Oct<T> *>(p + c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = up(o.e[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < n ? up(p[c + j]) : 0.0f;
+    }
+}
+
+// v, rounded once, to columns [c, c + 8) of the row at p, as far as they are below n
+template <class T>
+__device__ __forceinline__ void store8(T *p, int64_t c, int64_t n, const float (&v)[8]) {
+    Oct<T> o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o.e[j] = (T)v[j];
+    if (c + 8 <= n) {
+        *reinterpret_cast<Oct<T> *>(p + c) = o;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < n) p[c + j] = o.e[j];
+    }
+}
+
+// ---- dropout --------------------------------------------------------------------------
+
+// One block of Philox4x32-10: ten rounds of two 32 x 32 -> 64 bit products, the key
+// raised by two odd constants in between.
+__device__ __forceinline__ u4v philox(uint64_t key, uint64_t counter) {
+    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+    uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = 0, c3 = 0;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return u4v{c0, c1, c2, c3};
+}
+
+// Dropout of one call: 16 bits an element, so that a block serves the eight elements a
+// lane holds and the generator's ten rounds stay below the time of their memory traffic.
+struct Drop {
+    const uint64_t *rng = nullptr;   // device (seed, offset); null: no dropout
+    uint32_t threshold = 0;          // T: kept where the 16 bits are >= T (65536: nothing is)
+    float scale = 1.0f;              // 1 / (1 - T 2^-16)
+};
+
+// false: p is no probability, or rng is missing
+inline bool make_drop(float p, const uint64_t *rng, Drop *d) {
+    *d = Drop();
+    if (!(p >= 0.0f && p <= 1.0f)) return false;
+    d->threshold = (uint32_t)floor((double)p * 65536.0 + 0.5);
+    if (d->threshold == 0) return true;
+    if (!rng) return false;
+    d->rng = rng;
+    d->scale = d->threshold < 65536u ? (float)(65536.0 / (65536.0 - d->threshold)) : 0.0f;
+    return true;
+}
+
+// The seed and offset, read once by each thread.
+struct DropState {
+    uint64_t seed = 0, offset = 0, blocks_per_row = 0;
+    __device__ __forceinline__ void init(const Drop &d, int64_t cols) {
+        seed = d.rng[0];
+        offset = d.rng[1];
+        blocks_per_row = (uint64_t)((cols + 7) >> 3);
+    }
+    // the 128 bits of columns [c, c + 8) of row r, c a multiple of 8
+    __device__ __forceinline__ u4v bits(int64_t r, int64_t c) const {
+        return philox(seed, offset + (uint64_t)r * blocks_per_row + (uint64_t)(c >> 3));
+    }
+};
+
+// v of the eight columns of a block: what is dropped becomes 0 whatever it was
+__device__ __forceinline__ void drop8(u4v bits, uint32_t threshold, float scale, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = j & 1 ? bits[j >> 1] >> 16 : bits[j >> 1] & 0xFFFFu;
+        v[j] = u >= threshold ? v[j] * scale : 0.0f;
+    }
+}
+
+// ---- activations ------------------------------------------------------------------------
+
+// 1 / (1 + exp(-t))
+__device__ __forceinline__ float sigmoid(float t) { return 1.0f / (1.0f + expf(-t)); }
+
+constexpr float GELU_C = 1.5957691216057308f;   // 2 sqrt(2 / pi): z / (1 + exp(-C (z + 0.044715 z^3)))
+constexpr float GELU_A = 0.044715f;
+
+__device__ __forceinline__ float activate(int act, float z) {
+    switch (act) {
+    case MLP_ACT_RELU: return z < 0.0f ? 0.0f : z;   // a NaN passes
+    case MLP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    case MLP_ACT_GELU_TANH: return z * sigmoid(GELU_C * (z + GELU_A * z * z * z));
+    case MLP_ACT_SILU: return z * sigmoid(z);
+    }
+    return z;
+}
+
+// v a'(z); where ReLU masks, 0 whatever v is
+__device__ __forceinline__ float activate_back(int act, float z, float v) {
+    switch (act) {
+    case MLP_ACT_RELU: return z > 0.0f ? v : 0.0f;
+    case MLP_ACT_GELU:   // Phi(z) + z phi(z)
+        return v * (0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z));
+    case MLP_ACT_GELU_TANH: {
+        const float s = sigmoid(GELU_C * (z + GELU_A * z * z * z));
+        return v * (s + z * s * (1.0f - s) * GELU_C * (1.0f + 3.0f * GELU_A * z * z));
+    }
+    case MLP_ACT_SILU: {
+        const float s = sigmoid(z);
+        return v * (s * (1.0f + z * (1.0f - s)));
+    }
+    }
+    return v;
+}
+
+inline bool dtype_valid(int32_t t) { return t == MLP_F32 || t == MLP_BF16 || t == MLP_F16; }
+inline size_t dtype_bytes(int32_t t) { return t == MLP_F32 ? 4 : 2; }
+
+}  // namespace mlp

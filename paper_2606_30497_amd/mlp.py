@@ -36,7 +36,10 @@ EXPORTS = ("mlp_workspace_bytes", "mlp_init", "mlp_set_stream", "mlp_strategy_wo
            "mlp_deep_param_count", "mlp_deep_workspace_bytes", "mlp_deep_init", "mlp_deep_forward",
            "mlp_deep_backward", "mlp_deep_sgd_step", "mlp_deep_train_epochs",
            "mlp_deep_check_errors", "mlp_deep_profile", "mlp_deep_last_kernel_ms",
-           "mlp_deep_destroy")
+           "mlp_deep_destroy",
+           "mlp_linear_workspace_bytes", "mlp_linear_init", "mlp_linear_set_stream",
+           "mlp_linear_forward", "mlp_linear_backward", "mlp_linear_destroy",
+           "mlp_dropout_forward", "mlp_dropout_backward")
 
 
 class MLPError(RuntimeError):
@@ -104,6 +107,19 @@ def load(require_built: bool = True):
         "mlp_deep_profile": (ctypes.c_int, [_vp, _i32]),
         "mlp_deep_last_kernel_ms": (ctypes.c_int, [_vp, ctypes.POINTER(_f32)]),
         "mlp_deep_destroy": (None, [_vp]),
+        "mlp_linear_workspace_bytes": (ctypes.c_size_t, [_i32, _i64, _i64, _i64]),
+        "mlp_linear_init": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i64, _i64, _i32, _i64, _vp,
+                                           _vp, _vp, ctypes.c_size_t, _vp]),
+        "mlp_linear_set_stream": (ctypes.c_int, [_vp, _vp]),
+        "mlp_linear_forward": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _f32, _vp, _vp, _i64,
+                                              _vp, _i64]),
+        "mlp_linear_backward": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _f32, _vp,
+                                               _vp, _i64, _vp, _vp]),
+        "mlp_linear_destroy": (None, [_vp]),
+        "mlp_dropout_forward": (ctypes.c_int, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _vp,
+                                               _i64, _vp]),
+        "mlp_dropout_backward": (ctypes.c_int, [_i32, _i64, _i64, _vp, _i64, _f32, _vp, _vp, _i64,
+                                                _vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -441,3 +457,205 @@ def mlp_deep_last_kernel_ms(ctx: DeepContext) -> float:
     ms = _f32(0.0)
     _check("mlp_deep_last_kernel_ms", load().mlp_deep_last_kernel_ms(ctx.handle, ctypes.byref(ms)))
     return float(ms.value)
+
+
+# --- layers: a dense layer and dropout -------------------------------------------
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _mat(t, name, dtype, device, rows, cols):
+    """(pointer, row stride) of a [rows, cols] matrix whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError("%s must be [%d, %d], is %s" % (name, rows, cols, list(t.shape)))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row of %s must be adjacent" % name)
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError("the rows of %s overlap" % name)
+    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+
+
+def _vec(t, name, dtype, device, n):
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    if t.numel() != n:
+        raise ValueError("%s has %d elements, needs %d" % (name, t.numel(), n))
+    return _dev(t, name, dtype=dtype)
+
+
+def _rng(rng, device):
+    """The generator's state: int64 [2] (seed, offset) in device memory."""
+    return _vec(rng, "rng", torch.int64, device, 2)
+
+
+class LinearContext:
+    """A dense layer's context bound to caller-owned W, bias and workspace."""
+
+    def __init__(self, handle, W, bias, workspace, activation, max_rows, stream):
+        self.handle = handle
+        self.W, self.bias, self.workspace = W, bias, workspace
+        self.d_in, self.d_out = W.shape
+        self.activation, self.max_rows = activation, max_rows
+        self.stream = stream    # None: each call goes on the current stream
+        self.bound = stream     # the stream the library's context is on
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.mlp_linear_destroy(h)
+
+
+def mlp_linear_workspace_bytes(dtype: torch.dtype, d_in: int, d_out: int, max_rows: int) -> int:
+    return int(load().mlp_linear_workspace_bytes(DTYPES[dtype], d_in, d_out, max_rows))
+
+
+def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_BATCH, workspace=None,
+                    stream=None) -> LinearContext:
+    """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
+    bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS. Calls
+    go on `stream`, or on the current stream at each call where none is given."""
+    lib = load()
+    if W.dim() != 2:
+        raise ValueError("W must be [d_in, d_out]")
+    if W.dtype not in DTYPES:
+        raise TypeError("W must be one of %s" % (tuple(DTYPES),))
+    d_in, d_out = W.shape
+    wp = _dev(W, "W", dtype=W.dtype)
+    bp = _vec(bias, "bias", W.dtype, W.device, d_out)
+    need = mlp_linear_workspace_bytes(W.dtype, d_in, d_out, max_rows)
+    if need == 0:
+        raise MLPError("mlp_linear_workspace_bytes", -2)
+    with torch.cuda.device(W.device):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=W.device)
+        if workspace.device != W.device:
+            raise ValueError("workspace is on %s, not on %s" % (workspace.device, W.device))
+        _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
+        handle = _vp()
+        _check("mlp_linear_init",
+               lib.mlp_linear_init(ctypes.byref(handle), DTYPES[W.dtype], d_in, d_out,
+                                   ACTIVATIONS[activation], max_rows, wp, bp, workspace.data_ptr(),
+                                   workspace.numel(), stream or 0))
+    return LinearContext(handle, W, bias, workspace, activation, max_rows, stream)
+
+
+def mlp_linear_set_stream(ctx: LinearContext, stream) -> None:
+    """Later calls go on `stream` (None: on the current stream at each call)."""
+    _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, stream or 0))
+    ctx.stream, ctx.bound = stream, stream
+
+
+def _bind_stream(ctx):
+    """Put the context on the current stream where it has none of its own."""
+    if ctx.stream is None:
+        s = torch.cuda.current_stream(ctx.W.device).cuda_stream
+        if s != ctx.bound:
+            _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, s))
+            ctx.bound = s
+
+
+def _new(ctx, *shape):
+    """An output of the context's type, its memory taken on the stream that writes it."""
+    if ctx.stream is None:
+        return torch.empty(shape, dtype=ctx.W.dtype, device=ctx.W.device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.W.device)):
+        return torch.empty(shape, dtype=ctx.W.dtype, device=ctx.W.device)
+
+
+def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, out=None, z=None,
+                       save_z=False):
+    """Y = residual + dropout(a(X W + bias)); with save_z (or a tensor z) also z = X W +
+    bias, which the backward call takes: then (Y, z) is returned."""
+    if X.dim() != 2:
+        raise ValueError("X must be [rows, d_in]")
+    W, rows, n = ctx.W, X.shape[0], ctx.d_out
+    dev, dt = W.device, W.dtype
+    xp, ldx = _mat(X, "X", dt, dev, rows, ctx.d_in)
+    rp, ldr = _mat(residual, "residual", dt, dev, rows, n)
+    gp = _rng(rng, dev)
+    if out is None:
+        out = _new(ctx, rows, n)
+    if z is None and save_z:
+        z = _new(ctx, rows, n)
+    yp, ldy = _mat(out, "out", dt, dev, rows, n)
+    zp, ldz = _mat(z, "z", dt, dev, rows, n)
+    _bind_stream(ctx)
+    _check("mlp_linear_forward", load().mlp_linear_forward(ctx.handle, xp, ldx, rows, rp, ldr, float(p),
+                                                           gp, yp, ldy, zp, ldz))
+    return out if z is None else (out, z)
+
+
+def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need_dx=True, need_dw=True,
+                        need_db=True, dX=None, dW=None, db=None):
+    """(dX, dW, db) of a forward call with the same X, p and rng; None for what is not
+    needed (db: for a layer without bias). X may be None where dW is not needed."""
+    if dY.dim() != 2:
+        raise ValueError("dY must be [rows, d_out]")
+    W, rows, n = ctx.W, dY.shape[0], ctx.d_out
+    dev, dt = W.device, W.dtype
+    xp, ldx = _mat(X, "X", dt, dev, rows, ctx.d_in)
+    gyp, lddy = _mat(dY, "dY", dt, dev, rows, n)
+    zp, ldz = _mat(z, "z", dt, dev, rows, n)
+    gp = _rng(rng, dev)
+    if dX is None and need_dx:
+        dX = _new(ctx, rows, ctx.d_in)
+    if dW is None and need_dw:
+        dW = _new(ctx, ctx.d_in, n)
+    if db is None and need_db and ctx.bias is not None:
+        db = _new(ctx, n)
+    dxp, lddx = _mat(dX, "dX", dt, dev, rows, ctx.d_in)
+    dwp = _vec(dW, "dW", dt, dev, ctx.d_in * n)
+    dbp = _vec(db, "db", dt, dev, n)
+    _bind_stream(ctx)
+    _check("mlp_linear_backward",
+           load().mlp_linear_backward(ctx.handle, xp, ldx, zp, ldz, gyp, lddy, rows, float(p), gp, dxp,
+                                      lddx, dwp, dbp))
+    return dX, dW, db
+
+
+def _dropout_call(fn, X, p, rng, residual, out, name):
+    if X.dim() != 2:
+        raise ValueError("%s must be [rows, cols]" % name)
+    if X.dtype not in DTYPES:
+        raise TypeError("%s must be one of %s" % (name, tuple(DTYPES)))
+    rows, cols = X.shape
+    dev, dt = X.device, X.dtype
+    xp, ldx = _mat(X, name, dt, dev, rows, cols)
+    rp, ldr = _mat(residual, "residual", dt, dev, rows, cols)
+    gp = _rng(rng, dev)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=dt, device=dev)
+    yp, ldy = _mat(out, "out", dt, dev, rows, cols)
+    args = (xp, ldx, float(p), gp, yp, ldy)
+    if fn == "mlp_dropout_forward":
+        args = (xp, ldx, rp, ldr, float(p), gp, yp, ldy)
+    f, s = getattr(load(), fn), torch.cuda.current_stream(dev).cuda_stream
+    if dev.index == torch.cuda.current_device():
+        st = f(DTYPES[dt], rows, cols, *args, s)
+    else:
+        with torch.cuda.device(dev):
+            st = f(DTYPES[dt], rows, cols, *args, s)
+    _check(fn, st)
+    return out
+
+
+def mlp_dropout_forward(X, p, rng, residual=None, out=None):
+    """residual + dropout(X) on the current stream of X's device; rng int64 [2] (seed,
+    offset) in device memory. out may be X or residual."""
+    return _dropout_call("mlp_dropout_forward", X, p, rng, residual, out, "X")
+
+
+def mlp_dropout_backward(dY, p, rng, out=None):
+    """The gradient of mlp_dropout_forward with the same p and rng; out may be dY."""
+    return _dropout_call("mlp_dropout_backward", dY, p, rng, None, out, "dY")

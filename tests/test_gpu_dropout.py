@@ -1,0 +1,171 @@
+"""mlp_dropout_forward / mlp_dropout_backward against the element-by-element definition."""
+import numpy as np
+import pytest
+import torch
+
+from tests import layers_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mlp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2606_30497_amd import mlp as m
+    m.load(require_built=True)
+    return m
+
+
+def _rng(seed, offset):
+    def s64(v):
+        v &= (1 << 64) - 1
+        return v - (1 << 64) if v >> 63 else v
+    return torch.tensor([s64(seed), s64(offset)], dtype=torch.int64, device="cuda")
+
+
+def _rows(g, rows, cols, dtype, pad, fill=7.0):
+    """A [rows, cols] view, its rows pad elements apart, of a buffer of fill values."""
+    buf = torch.full((rows, cols + pad), fill, dtype=R.DTYPES[dtype], device="cuda")
+    v = buf[:, :cols]
+    v.copy_(torch.randn(rows, cols, generator=g).to(R.DTYPES[dtype]))
+    return buf, v
+
+
+def _check(got, x, r, rng, p, dtype):
+    f = R.factor(rng, x.shape[0], x.shape[1], p)
+    y = x.cpu().double() * f
+    b = 2 * R.E * y.abs()
+    if r is not None:
+        y = y + r.cpu().double()
+        b = b + 2 * R.E * (y.abs() + r.cpu().double().abs())
+    R.check("dropout", got, y, b + R.U[dtype] * y.abs() + R.TINY[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 7, 0), (3, 8, 0), (5, 9, 1), (64, 1001, 3), (7, 4096, 8),
+                                           (1000, 33, 0), (2050, 1, 2), (513, 520, 13)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_forward(mlp, dtype, rows, cols, pad, residual):
+    print(dtype, rows, cols, pad, residual, flush=True)
+    g = torch.Generator().manual_seed(rows + cols)
+    _, x = _rows(g, rows, cols, dtype, pad)
+    r = _rows(g, rows, cols, dtype, 2 * pad)[1] if residual else None
+    buf, out = _rows(g, rows, cols, dtype, pad + 1)
+    rng, p = (0x1234567887654321, (1 << 32) - 2), 0.3   # the counter passes 32 bits
+    got = mlp.mlp_dropout_forward(x, p, _rng(*rng), residual=r, out=out)
+    torch.cuda.synchronize()
+    _check(got, x, r, rng, p, dtype)
+    assert bool((buf[:, cols:] == 7.0).all())   # between the rows nothing is written
+    # whole tensors give the same values as rows apart
+    again = mlp.mlp_dropout_forward(x.contiguous(), p, _rng(*rng), residual=None if r is None else r.contiguous())
+    assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("p", [0.0, 1e-6, 2.0 ** -16, 0.1, 0.5, 0.99999, 1.0])
+def test_probabilities(mlp, dtype, p):
+    g = torch.Generator().manual_seed(3)
+    _, x = _rows(g, 129, 250, dtype, 0)
+    rng = (99, 1 << 63)
+    got = mlp.mlp_dropout_forward(x, p, _rng(*rng))
+    _check(got, x, None, rng, p, dtype)
+    assert torch.equal(mlp.mlp_dropout_backward(x, p, _rng(*rng)), got)
+    if R.threshold(p) == 0:
+        assert torch.equal(got, x) and torch.equal(mlp.mlp_dropout_forward(x, p, None), x)
+
+
+def test_counter_wraps(mlp):
+    g = torch.Generator().manual_seed(4)
+    _, x = _rows(g, 40, 100, "f32", 0)
+    rng = (-1, (1 << 64) - 100)
+    _check(mlp.mlp_dropout_forward(x, 0.5, _rng(*rng)), x, None, rng, 0.5, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_dropped_values_are_zero_whatever_they_were(mlp, dtype):
+    x = torch.full((64, 96), float("nan"), dtype=R.DTYPES[dtype], device="cuda")
+    x[32:] = float("inf")
+    keep = torch.from_numpy(R.keep_mask(8, 0, 64, 96, 0.5)).cuda()
+    y = mlp.mlp_dropout_forward(x, 0.5, _rng(8, 0))
+    assert bool((y[~keep] == 0).all()) and bool(y[:32][keep[:32]].isnan().all()) and bool((y[32:][keep[32:]] == float("inf")).all())
+
+
+def test_in_place(mlp):
+    g = torch.Generator().manual_seed(5)
+    _, x = _rows(g, 300, 77, "bf16", 5)
+    _, r = _rows(g, 300, 77, "bf16", 3)
+    want = mlp.mlp_dropout_forward(x, 0.2, _rng(1, 2), residual=r)
+    res = r.clone()
+    assert torch.equal(mlp.mlp_dropout_forward(x, 0.2, _rng(1, 2), residual=res, out=res), want)
+    grad = mlp.mlp_dropout_backward(x, 0.2, _rng(1, 2))
+    assert mlp.mlp_dropout_forward(x, 0.2, _rng(1, 2), residual=r, out=x) is x
+    assert torch.equal(x, want)
+    x2 = r.clone()
+    want = mlp.mlp_dropout_backward(r, 0.2, _rng(1, 2))
+    assert torch.equal(mlp.mlp_dropout_backward(x2, 0.2, _rng(1, 2), out=x2), want)
+    assert grad.shape == want.shape
+
+
+def test_empty(mlp):
+    for shape in ((0, 8), (8, 0), (0, 0)):
+        x = torch.empty(*shape, device="cuda")
+        assert mlp.mlp_dropout_forward(x, 0.5, _rng(1, 2)).shape == x.shape
+
+
+def test_offsets_past_32_bits(mlp):
+    """Rows so far apart that the last ones start past 2^32 elements."""
+    rows, cols, ld = 70_000, 24, 65_536
+    x = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)[:, 100:100 + cols]
+    x.copy_(torch.randn(rows, cols, device="cuda"))
+    got = mlp.mlp_dropout_forward(x, 0.3, _rng(1, 2), out=torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda"))
+    _check(got, x, None, (1, 2), 0.3, "bf16")
+
+
+def test_captured_calls_draw_new_masks(mlp):
+    """A replay reads the generator's state when it runs: with the offset moved on in
+    between, each replay draws the mask of its own offset."""
+    g = torch.Generator().manual_seed(6)
+    _, x = _rows(g, 64, 200, "bf16", 0)
+    rng, out = _rng(7, 0), torch.empty(64, 200, dtype=torch.bfloat16, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        mlp.mlp_dropout_forward(x, 0.5, rng, out=out)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=s):
+            mlp.mlp_dropout_forward(x, 0.5, rng, out=out)
+        for k in range(4):
+            gr.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            _check(got, x, None, (7, 1600 * k), 0.5, "bf16")
+            assert torch.equal(mlp.mlp_dropout_forward(x, 0.5, rng), got)
+            rng[1] += 64 * 25     # rows * ceil(cols / 8) counters a call
+            torch.cuda.synchronize()
+
+
+def test_refusals(mlp):
+    x = torch.zeros(4, 8, device="cuda")
+    r = _rng(1, 2)
+    for p in (-0.1, 1.1, float("nan"), float("inf")):
+        with pytest.raises(mlp.MLPError):
+            mlp.mlp_dropout_forward(x, p, r)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_dropout_forward(x, 0.5, None)
+    with pytest.raises(TypeError):
+        mlp.mlp_dropout_forward(x.double(), 0.5, r)
+    with pytest.raises(TypeError):
+        mlp.mlp_dropout_forward(x, 0.5, r.int())
+    with pytest.raises(TypeError):
+        mlp.mlp_dropout_forward(x.cpu(), 0.5, r)
+    with pytest.raises(ValueError):
+        mlp.mlp_dropout_forward(x.t(), 0.5, r)
+    with pytest.raises(ValueError):
+        mlp.mlp_dropout_forward(x, 0.5, r, residual=x[:2])
+    with pytest.raises(ValueError):
+        mlp.mlp_dropout_forward(x[:1].expand(4, 8), 0.5, r, out=x[:1].expand(4, 8))
+    with pytest.raises(mlp.MLPError):   # the same memory at two strides
+        y = torch.zeros(64, device="cuda")
+        mlp.mlp_dropout_forward(y[:32].view(4, 8), 0.5, r, out=torch.as_strided(y, (4, 8), (16, 1)))
+    assert float(x.abs().max()) == 0.0

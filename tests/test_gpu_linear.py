@@ -1,0 +1,296 @@
+"""mlp_linear_forward / mlp_linear_backward against the 64-bit definition."""
+import pytest
+import torch
+
+from tests import layers_ref as R
+from tests.test_gpu_dropout import _rng, _rows, mlp  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# (rows, d_in, d_out, pad): one row to many, widths of one, odd ones, whole tiles
+SHAPES = [(1, 1, 1, 0), (1, 32, 1, 0), (2, 5, 7, 3), (1, 256, 512, 0), (1, 1000, 1001, 1), (3, 2048, 40, 0),
+          (8, 64, 4097, 0), (15, 777, 64, 2), (16, 512, 256, 8), (17, 33, 9, 0), (31, 1024, 130, 0), (32, 100, 264, 4),
+          (33, 17, 2049, 5), (48, 520, 520, 0), (64, 256, 256, 0), (65, 255, 257, 0), (100, 1032, 72, 8),
+          (128, 128, 128, 0), (129, 64, 1, 0), (200, 2056, 136, 0), (256, 512, 384, 0), (257, 96, 520, 16),
+          (300, 513, 77, 1), (512, 1024, 256, 0), (1000, 40, 8, 0), (777, 136, 1000, 8), (1500, 8, 24, 0),
+          (2000, 264, 264, 0)]
+# activation, p, bias, residual, z kept
+OPTIONS = [("none", 0.0, False, False, False), ("relu", 0.0, True, True, True), ("gelu", 0.1, True, False, True),
+           ("gelu_tanh", 0.5, False, True, False), ("silu", 0.3, True, True, True)]
+
+
+def _layer(g, d_in, d_out, dtype, bias):
+    W = (torch.randn(d_in, d_out, generator=g) * (2.0 / d_in) ** 0.5).to(R.DTYPES[dtype]).cuda()
+    return W, (torch.randn(d_out, generator=g).to(R.DTYPES[dtype]).cuda() if bias else None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,d_in,d_out,pad", SHAPES)
+def test_forward(mlp, dtype, rows, d_in, d_out, pad):  # noqa: F811
+    i = SHAPES.index((rows, d_in, d_out, pad)) + sorted(R.DTYPES).index(dtype)
+    for act, p, bias, residual, keep_z in (OPTIONS[i % 5], OPTIONS[(i + 2) % 5]):
+        print(dtype, rows, d_in, d_out, pad, act, p, bias, residual, keep_z, flush=True)
+        g = torch.Generator().manual_seed(100 + i)
+        W, b = _layer(g, d_in, d_out, dtype, bias)
+        _, x = _rows(g, rows, d_in, dtype, pad, float("nan"))
+        r = _rows(g, rows, d_out, dtype, pad, float("nan"))[1] if residual else None
+        ybuf, y = _rows(g, rows, d_out, dtype, pad + 2)
+        zbuf, z = _rows(g, rows, d_out, dtype, pad)
+        ctx = mlp.mlp_linear_init(W, b, act, max_rows=rows)
+        rng = (77, (1 << 32) - 5)
+        mlp.mlp_linear_forward(ctx, x, residual=r, p=p, rng=_rng(*rng), out=y, z=z if keep_z else None)
+        torch.cuda.synchronize()
+        ry, rz, by, bz = R.forward(x, W, b, r, act, p, rng, dtype)
+        R.check("y", y, ry, by)
+        if keep_z:
+            R.check("z", z, rz, bz)
+        assert bool((ybuf[:, d_out:] == 7.0).all()) and bool((zbuf[:, d_out:] == 7.0).all())
+        # contiguous tensors, and a second call, give the same bits
+        y2 = mlp.mlp_linear_forward(ctx, x.contiguous(), residual=None if r is None else r.contiguous(), p=p,
+                                    rng=_rng(*rng))
+        assert torch.equal(y2, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,d_in,d_out,pad", SHAPES)
+def test_backward(mlp, dtype, rows, d_in, d_out, pad):  # noqa: F811
+    i = SHAPES.index((rows, d_in, d_out, pad)) + sorted(R.DTYPES).index(dtype)
+    for act, p, bias, _, _ in (OPTIONS[i % 5], OPTIONS[(i + 3) % 5]):
+        print(dtype, rows, d_in, d_out, pad, act, p, bias, flush=True)
+        g = torch.Generator().manual_seed(200 + i)
+        W, b = _layer(g, d_in, d_out, dtype, bias)
+        _, x = _rows(g, rows, d_in, dtype, pad, float("nan"))
+        _, z = _rows(g, rows, d_out, dtype, pad + 1, float("nan"))
+        _, dy = _rows(g, rows, d_out, dtype, pad, float("nan"))
+        dxbuf, dx = _rows(g, rows, d_in, dtype, pad + 3)
+        ctx = mlp.mlp_linear_init(W, b, act, max_rows=rows)
+        rng = (78, -3)
+        _, dw, db = mlp.mlp_linear_backward(ctx, x, dy, z=None if act == "none" else z, p=p, rng=_rng(*rng), dX=dx)
+        torch.cuda.synchronize()
+        ref, bound = R.backward(x, W, z, dy, act, p, rng, dtype)
+        R.check("dx", dx, ref["dx"], bound["dx"])
+        R.check("dw", dw, ref["dw"], bound["dw"])
+        assert bool((dxbuf[:, d_in:] == 7.0).all()) and (db is None) == (b is None)
+        if db is not None:
+            R.check("db", db, ref["db"], bound["db"])
+        # each gradient alone, from contiguous tensors, and again: the same bits
+        cx, cz, cdy = x.contiguous(), None if act == "none" else z.contiguous(), dy.contiguous()
+        for need in ("dx", "dw", "db"):
+            out = mlp.mlp_linear_backward(ctx, cx if need == "dw" else None, cdy, z=cz, p=p, rng=_rng(*rng),
+                                          need_dx=need == "dx", need_dw=need == "dw", need_db=need == "db")
+            for name, got, want in zip(("dx", "dw", "db"), out, (dx, dw, db)):
+                assert (got is None) == (name != need or want is None)
+                assert got is None or torch.equal(got, want), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_rows(mlp, dtype):  # noqa: F811
+    g = torch.Generator().manual_seed(1)
+    W, b = _layer(g, 40, 24, dtype, True)
+    ctx = mlp.mlp_linear_init(W, b, "relu", max_rows=64)
+    e = W.new_empty
+    assert mlp.mlp_linear_forward(ctx, e(0, 40)).shape == (0, 24)
+    dx, dw, db = mlp.mlp_linear_backward(ctx, e(0, 40), e(0, 24), z=e(0, 24), dW=torch.full_like(W, 3), db=torch.full_like(b, 3))
+    assert dx.shape == (0, 40) and float(dw.abs().max()) == 0 and float(db.abs().max()) == 0
+
+
+@pytest.mark.parametrize("rows", [1, 40, 600])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_dropout_of_the_layer_is_dropout(mlp, dtype, rows):  # noqa: F811
+    """The layer's mask is that of mlp_dropout_forward with the same state and shape."""
+    g = torch.Generator().manual_seed(2)
+    W, b = _layer(g, 64, 203, dtype, True)
+    _, x = _rows(g, rows, 64, dtype, 0)
+    ctx = mlp.mlp_linear_init(W, b, "none", max_rows=rows)
+    y = mlp.mlp_linear_forward(ctx, x, p=0.4, rng=_rng(3, 4))
+    ones = torch.ones(rows, 203, device="cuda")
+    assert torch.equal(y != 0, mlp.mlp_dropout_forward(ones, 0.4, _rng(3, 4)) != 0)
+    # the backward call's too
+    _, _, db = mlp.mlp_linear_backward(ctx, x, ones.to(W.dtype), p=0.4, rng=_rng(3, 4), need_dx=False, need_dw=False)
+    ref = (torch.from_numpy(R.keep_mask(3, 4, rows, 203, 0.4)).double() * R.drop_scale(0.4)).sum(0)
+    e = 4 * R.E * (rows + 32) ** 0.5 * ref + R.U[dtype] * ref
+    R.check("db", db, ref, e)
+
+
+def test_residual_in_place_and_masked_values(mlp):  # noqa: F811
+    g = torch.Generator().manual_seed(3)
+    W, b = _layer(g, 72, 48, "bf16", True)
+    _, x = _rows(g, 130, 72, "bf16", 0)
+    _, r = _rows(g, 130, 48, "bf16", 6)
+    ctx = mlp.mlp_linear_init(W, b, "relu", max_rows=130)
+    want = mlp.mlp_linear_forward(ctx, x, residual=r)
+    got = mlp.mlp_linear_forward(ctx, x, residual=r, out=r)
+    assert got is r and torch.equal(got, want)
+    # gradients: what ReLU masks or dropout drops is 0, also where dY is not finite
+    _, z = _rows(g, 130, 48, "bf16", 0)
+    keep = torch.from_numpy(R.keep_mask(5, 6, 130, 48, 0.5)).cuda()
+    dy = torch.where((z > 0) & keep, torch.randn(130, 48, device="cuda").to(z.dtype), torch.tensor(float("nan"), dtype=z.dtype, device="cuda"))
+    dx, dw, db = mlp.mlp_linear_backward(ctx, x, dy, z=z, p=0.5, rng=_rng(5, 6))
+    ref, bound = R.backward(x, W, z, torch.nan_to_num(dy), "relu", 0.5, (5, 6), "bf16")
+    for n, t in (("dx", dx), ("dw", dw), ("db", db)):
+        R.check(n, t, ref[n], bound[n])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_past_32_bits(mlp, dtype):  # noqa: F811
+    """X, Y, Z and dY whose rows are so far apart that the last start past 2^32 bytes
+    (fp32) and 2^31 elements."""
+    rows, d_in, d_out, ld = 600, 40, 24, 1 << 22
+    g = torch.Generator().manual_seed(4)
+    W, b = _layer(g, d_in, d_out, dtype, True)
+
+    def far(cols):
+        t = torch.empty(rows * ld, dtype=W.dtype, device="cuda").view(rows, ld)[:, 8:8 + cols]
+        t.copy_(torch.randn(rows, cols, generator=g))
+        return t
+
+    x, y, z, dy = far(d_in), far(d_out), far(d_out), far(d_out)
+    ctx = mlp.mlp_linear_init(W, b, "silu", max_rows=rows)
+    mlp.mlp_linear_forward(ctx, x, out=y, z=z)
+    ry, rz, by, bz = R.forward(x, W, b, None, "silu", 0.0, None, dtype)
+    R.check("y", y, ry, by)
+    R.check("z", z, rz, bz)
+    dx, dw, db = mlp.mlp_linear_backward(ctx, x, dy, z=z)
+    ref, bound = R.backward(x, W, z, dy, "silu", 0.0, None, dtype)
+    R.check("dx", dx, ref["dx"], bound["dx"])
+    R.check("dw", dw, ref["dw"], bound["dw"])
+    R.check("db", db, ref["db"], bound["db"])
+
+
+def test_fewer_rows_than_the_context_has_room_for(mlp):  # noqa: F811
+    g = torch.Generator().manual_seed(5)
+    W, b = _layer(g, 264, 136, "bf16", True)
+    big = mlp.mlp_linear_init(W, b, "gelu", max_rows=3000)
+    for rows in (1, 20, 130, 700, 3000):
+        _, x = _rows(g, rows, 264, "bf16", 0)
+        _, dy = _rows(g, rows, 136, "bf16", 0)
+        small = mlp.mlp_linear_init(W, b, "gelu", max_rows=rows)
+        ry, rz, by, bz = R.forward(x, W, b, None, "gelu", 0.0, None, "bf16")
+        for ctx in (big, small):
+            y, z = mlp.mlp_linear_forward(ctx, x, save_z=True)
+            R.check("y", y, ry, by)
+            grads = mlp.mlp_linear_backward(ctx, x, dy, z=z)
+            ref, bound = R.backward(x, W, z, dy, "gelu", 0.0, None, "bf16")
+            for n, t in zip(("dx", "dw", "db"), grads):
+                R.check(n, t, ref[n], bound[n])
+
+
+def _block_loss(mlp, ctx1, ctx2, x, dy, rng):  # noqa: F811
+    """One residual block x + dropout(gelu(x W1 + b1) W2 + b2) forward and backward;
+    returns y and the gradients, dx with the residual's."""
+    h, z1 = mlp.mlp_linear_forward(ctx1, x, save_z=True)
+    y = mlp.mlp_linear_forward(ctx2, h, residual=x, p=0.1, rng=rng)
+    dh, dw2, db2 = mlp.mlp_linear_backward(ctx2, h, dy, p=0.1, rng=rng)
+    dx, dw1, db1 = mlp.mlp_linear_backward(ctx1, x, dh, z=z1)
+    return y, dx + dy, dw1, db1, dw2, db2
+
+
+@pytest.mark.parametrize("rows,d,f", [(37, 96, 200), (400, 128, 512)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_residual_block_and_its_graph(mlp, dtype, rows, d, f):  # noqa: F811
+    """Two layers together as a residual block is trained, against 64-bit autograd; then
+    recorded into a graph whose replays, with eager calls on the same contexts between
+    them, give the eager bits for the state they find."""
+    g = torch.Generator().manual_seed(rows)
+    W1, b1 = _layer(g, d, f, dtype, True)
+    W2, b2 = _layer(g, f, d, dtype, True)
+    _, x = _rows(g, rows, d, dtype, 0)
+    _, dy = _rows(g, rows, d, dtype, 0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        rng = _rng(21, 5)
+        ctx1 = mlp.mlp_linear_init(W1, b1, "gelu", max_rows=rows)
+        ctx2 = mlp.mlp_linear_init(W2, b2, "none", max_rows=rows)
+        got = _block_loss(mlp, ctx1, ctx2, x, dy, rng)
+        torch.cuda.synchronize()
+        ps = [t.cpu().double().requires_grad_() for t in (x, W1, b1, W2, b2)]
+        h = R.act(ps[0] @ ps[1] + ps[2], "gelu")
+        y = ps[0] + (h @ ps[3] + ps[4]) * R.factor((21, 5), rows, d, 0.1)
+        y.backward(dy.cpu().double())
+        # normwise: each of at most four roundings to the type on the way (h, z, dh, g)
+        # and the result's, u each at most, and the products' own sums
+        bar = 6 * R.U[dtype] + 64 * R.E
+        for name, a, b in zip(("y", "dx", "dW1", "db1", "dW2", "db2"), got, [y] + [t.grad for t in ps]):
+            e = float((a.cpu().double() - b.detach()).norm() / b.detach().norm())
+            print("%-4s %.2e (bar %.1e)" % (name, e, bar), flush=True)
+            assert e <= bar, name
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=s):
+            held = _block_loss(mlp, ctx1, ctx2, x, dy, rng)
+        for k in range(4):
+            gr.replay()
+            torch.cuda.synchronize()
+            replayed = [t.clone() for t in held]
+            eager = _block_loss(mlp, ctx1, ctx2, x, dy, rng)
+            torch.cuda.synchronize()
+            for a, b in zip(replayed, eager):
+                assert torch.equal(a, b)
+            rng[1] += 1000
+            x.mul_(-0.5)
+            torch.cuda.synchronize()
+
+
+def test_own_stream(mlp):  # noqa: F811
+    """A context with a stream of its own, called while another stream is current."""
+    g = torch.Generator().manual_seed(6)
+    W, b = _layer(g, 128, 256, "bf16", True)
+    _, x = _rows(g, 500, 128, "bf16", 0)
+    _, dy = _rows(g, 500, 256, "bf16", 0)
+    plain = mlp.mlp_linear_init(W, b, "silu", max_rows=500)
+    want = mlp.mlp_linear_forward(plain, x, save_z=True)
+    wantg = mlp.mlp_linear_backward(plain, x, dy, z=want[1])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    ctx = mlp.mlp_linear_init(W, b, "silu", max_rows=500, stream=s.cuda_stream)
+    for _ in range(3):
+        got = mlp.mlp_linear_forward(ctx, x, save_z=True)
+        gotg = mlp.mlp_linear_backward(ctx, x, dy, z=got[1])
+        s.synchronize()
+        for a, c in zip(got + gotg, want + wantg):
+            assert torch.equal(a, c)
+    mlp.mlp_linear_set_stream(ctx, None)
+    assert torch.equal(mlp.mlp_linear_forward(ctx, x), want[0])
+
+
+def test_refusals(mlp):  # noqa: F811
+    W = torch.zeros(16, 24, device="cuda")
+    b = torch.zeros(24, device="cuda")
+    ctx = mlp.mlp_linear_init(W, b, "relu", max_rows=8)
+    x, y = torch.zeros(8, 16, device="cuda"), torch.full((8, 24), 5.0, device="cuda")
+    z, r = torch.zeros(8, 24, device="cuda"), _rng(1, 2)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_forward(ctx, torch.zeros(9, 16, device="cuda"))
+    for p in (-0.5, 1.5, float("nan")):
+        with pytest.raises(mlp.MLPError):
+            mlp.mlp_linear_forward(ctx, x, p=p, rng=r, out=y)
+        with pytest.raises(mlp.MLPError):
+            mlp.mlp_linear_backward(ctx, x, y, z=z, p=p, rng=r)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_forward(ctx, x, p=0.5, out=y)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_forward(ctx, x, out=y, z=y)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_backward(ctx, x, y)                   # no z
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_backward(ctx, None, y, z=z)           # dW without X
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_backward(ctx, x, y, z=z, dX=x)
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_backward(ctx, x, y, z=z, dW=W)
+    for bad in (x.bfloat16(), x.cpu(), x.double()):
+        with pytest.raises(TypeError):
+            mlp.mlp_linear_forward(ctx, bad, out=y)
+    for bad in (x[:, :8], x.t().contiguous().t(), x[:1].expand(8, 16)):
+        with pytest.raises(ValueError):
+            mlp.mlp_linear_forward(ctx, bad, out=y)
+    with pytest.raises(ValueError):
+        mlp.mlp_linear_init(W, b[:8], "relu", max_rows=8)
+    with pytest.raises(ValueError):
+        mlp.mlp_linear_init(W, b, "relu", max_rows=8, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(KeyError):
+        mlp.mlp_linear_init(W, b, "swish", max_rows=8)
+    with pytest.raises(TypeError):
+        mlp.mlp_linear_init(W.double(), None, "relu", max_rows=8)
+    torch.cuda.synchronize()
+    assert bool((y == 5.0).all())
