@@ -128,32 +128,56 @@ __device__ __forceinline__ float sigmoid(float t) { return 1.0f / (1.0f + expf(-
 constexpr float GELU_C = 1.5957691216057308f;   // 2 sqrt(2 / pi): z / (1 + exp(-C (z + 0.044715 z^3)))
 constexpr float GELU_A = 0.044715f;
 
-__device__ __forceinline__ float activate(int act, float z) {
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.0f + erff(z * 0.70710678f)); }
+
+// v <- a(v)
+__device__ __forceinline__ void activate8(int act, float (&v)[8]) {
     switch (act) {
-    case MLP_ACT_RELU: return z < 0.0f ? 0.0f : z;   // a NaN passes
-    case MLP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    case MLP_ACT_GELU_TANH: return z * sigmoid(GELU_C * (z + GELU_A * z * z * z));
-    case MLP_ACT_SILU: return z * sigmoid(z);
+    case MLP_ACT_RELU:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];   // a NaN passes
+        break;
+    case MLP_ACT_GELU:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= normal_cdf(v[j]);
+        break;
+    case MLP_ACT_GELU_TANH:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= sigmoid(GELU_C * (v[j] + GELU_A * v[j] * v[j] * v[j]));
+        break;
+    case MLP_ACT_SILU:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]);
+        break;
     }
-    return z;
 }
 
-// v a'(z); where ReLU masks, 0 whatever v is
-__device__ __forceinline__ float activate_back(int act, float z, float v) {
+// v <- v a'(z); where ReLU masks, 0 whatever v is
+__device__ __forceinline__ void activate_back8(int act, const float (&z)[8], float (&v)[8]) {
     switch (act) {
-    case MLP_ACT_RELU: return z > 0.0f ? v : 0.0f;
+    case MLP_ACT_RELU:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = z[j] > 0.0f ? v[j] : 0.0f;
+        break;
     case MLP_ACT_GELU:   // Phi(z) + z phi(z)
-        return v * (0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z));
-    case MLP_ACT_GELU_TANH: {
-        const float s = sigmoid(GELU_C * (z + GELU_A * z * z * z));
-        return v * (s + z * s * (1.0f - s) * GELU_C * (1.0f + 3.0f * GELU_A * z * z));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= normal_cdf(z[j]) + z[j] * 0.39894228f * expf(-0.5f * z[j] * z[j]);
+        break;
+    case MLP_ACT_GELU_TANH:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = sigmoid(GELU_C * (z[j] + GELU_A * z[j] * z[j] * z[j]));
+            v[j] *= s + z[j] * s * (1.0f - s) * GELU_C * (1.0f + 3.0f * GELU_A * z[j] * z[j]);
+        }
+        break;
+    case MLP_ACT_SILU:
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = sigmoid(z[j]);
+            v[j] *= s * (1.0f + z[j] * (1.0f - s));
+        }
+        break;
     }
-    case MLP_ACT_SILU: {
-        const float s = sigmoid(z);
-        return v * (s * (1.0f + z * (1.0f - s)));
-    }
-    }
-    return v;
 }
 
 inline bool dtype_valid(int32_t t) { return t == MLP_F32 || t == MLP_BF16 || t == MLP_F16; }

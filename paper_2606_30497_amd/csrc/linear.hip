@@ -7,97 +7,60 @@
 #include <stdint.h>
 
 #include "layer.h"
+#include "linear_internal.h"
 
 namespace mlp {
 
 constexpr int64_t LINEAR_MAX_WIDTH = 1 << 20;
+constexpr int COL_CHUNKS = 256;                   // most row chunks of the column sums
+constexpr int64_t PART_FLOATS_MAX = 256 * 65536;  // 256 workgroups' tiles of partial sums
 
 struct LinearCtx {
     int32_t dtype = 0, act = 0;
     int64_t d_in = 0, d_out = 0, max_rows = 0;
     const void *W = nullptr, *bias = nullptr;
-    void *g = nullptr;          // [max_rows x ldg], the gradient in z
-    int64_t ldg = 0;
+    // workspace: operands as the matrix products take them (Operand): the gradient in z,
+    // and X and W where the caller's are not laid out so
+    uint16_t *g = nullptr, *x = nullptr, *w = nullptr;
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
+    float *part = nullptr;      // partial sums of the products
+    int64_t part_floats = 0;
     hipStream_t stream = nullptr;
     int device = 0;
 };
 
-constexpr int COL_CHUNKS = 256;
+static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 
-// A matrix product's epilogue: what becomes of the fp32 sums of one row's eight columns.
-struct Epilogue {
-    const void *bias, *R;
-    void *Z, *Y;
-    int64_t ldr, ldz, ldy;
-    int act;
-    Drop drop;
-};
-
+// v as an operand's elements [c, c + 8) of a row: rounded to the 16-bit type, or the
+// three bf16 parts of fp32, `plane` apart
 template <class T>
-__device__ __forceinline__ void finish8(const Epilogue &e, const DropState &st, int64_t r, int64_t c,
-                                        int64_t n, float (&v)[8]) {
-    if (e.bias) {
-        float b[8];
-        load8((const T *)e.bias, c, n, b);
+__device__ __forceinline__ void put8(uint16_t *p, int64_t plane, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        Oct<T> o;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += b[j];
-    }
-    if (e.Z) store8((T *)e.Z + r * e.ldz, c, n, v);
-    if (e.act != MLP_ACT_NONE) {
+        for (int j = 0; j < 8; ++j) o.e[j] = (T)v[j];
+        *reinterpret_cast<u4v *>(p) = __builtin_bit_cast(u4v, o);
+    } else {
+        uint32_t w[4][3];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = activate(e.act, v[j]);
-    }
-    if (e.drop.rng) drop8(st.bits(r, c), e.drop.threshold, e.drop.scale, v);
-    if (e.R) {
-        float q[8];
-        load8((const T *)e.R + r * e.ldr, c, n, q);
+        for (int j = 0; j < 4; ++j) split_pair(v[2 * j], v[2 * j + 1], w[j]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += q[j];
+        for (int i = 0; i < 3; ++i)
+            *reinterpret_cast<u4v *>(p + i * plane) = u4v{w[0][i], w[1][i], w[2][i], w[3][i]};
     }
-    store8((T *)e.Y + r * e.ldy, c, n, v);
 }
 
-// C[m][n] = sum_k a(m, k) b(k, n), a(m, k) = A[m sam + k sak], b(k, n) = B[k sbk + n sbn],
-// then the epilogue. 64 x 64 outputs a workgroup, K in chunks of 16 staged in LDS, two
-// rows of eight columns a thread on the vector units.
-struct ProductArgs {
-    const void *A, *B;
-    int64_t sam, sak, sbk, sbn, M, N, K;
-    Epilogue e;
-};
-
+// A matrix of rows x cols laid out as an operand: rows of pad8(cols) elements, what pads
+// them zero. Read and written once, bound by memory (fp32: 10 bytes an element).
 template <class T>
-__global__ __launch_bounds__(256) void k_product(const ProductArgs a) {
-    __shared__ float As[16][65], Bs[16][65];
-    const int t = threadIdx.x;
-    const int64_t m0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
-    const T *A = (const T *)a.A, *B = (const T *)a.B;
-    const int tr = t >> 3, tc = (t & 7) * 8;
-    float acc[2][8] = {};
-    for (int64_t k0 = 0; k0 < a.K; k0 += 16) {
-        for (int i = t; i < 1024; i += 256) {
-            // the faster index along the operand's contiguous direction
-            const int ak = a.sak == 1 ? i & 15 : i >> 6, am = a.sak == 1 ? i >> 4 : i & 63;
-            const int bk = a.sbk == 1 ? i & 15 : i >> 6, bn = a.sbk == 1 ? i >> 4 : i & 63;
-            As[ak][am] = m0 + am < a.M && k0 + ak < a.K ? up(A[(m0 + am) * a.sam + (k0 + ak) * a.sak]) : 0.0f;
-            Bs[bk][bn] = n0 + bn < a.N && k0 + bk < a.K ? up(B[(k0 + bk) * a.sbk + (n0 + bn) * a.sbn]) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] += As[k][tr + 32 * i] * Bs[k][tc + j];
-        __syncthreads();
-    }
-    DropState st;
-    if (a.e.drop.rng) st.init(a.e.drop, a.N);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t m = m0 + tr + 32 * i;
-        if (m < a.M && n0 + tc < a.N) finish8<T>(a.e, st, m, n0 + tc, a.N, acc[i]);
+__global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t rows, int64_t cols, uint16_t *out,
+                                              int64_t plane) {
+    const int64_t blocks = (cols + 7) / 8, total = rows * blocks, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const int64_t r = i / blocks, c = (i - r * blocks) * 8;
+        float v[8];
+        load8(P + r * ld, c, cols, v);
+        put8<T>(out + i * 8, plane, v);
     }
 }
 
@@ -105,9 +68,9 @@ __global__ __launch_bounds__(256) void k_product(const ProductArgs a) {
 // and 8 * groups columns.
 struct GradArgs {
     const void *Z, *dY;
-    void *G;
+    uint16_t *G;              // nullable, an operand of rows of pad8(N)
     float *col;               // nullable [chunks x N]
-    int64_t ldz, lddy, ldg, M, N, chunk;   // chunk: rows of a workgroup
+    int64_t ldz, lddy, plane, M, N, chunk;   // chunk: rows of a workgroup
     int groups;               // a power of two up to 32
     int act;
     Drop drop;
@@ -119,7 +82,7 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
     const int t = threadIdx.x;
     const int64_t c = ((int64_t)blockIdx.y * a.groups + t % a.groups) * 8;
     const int64_t r0 = (int64_t)blockIdx.x * a.chunk;
-    const int64_t r1 = r0 + a.chunk < a.M ? r0 + a.chunk : a.M;
+    const int64_t r1 = r0 + a.chunk < a.M ? r0 + a.chunk : a.M, ldg = (a.N + 7) / 8 * 8;
     DropState st;
     if (a.drop.rng) st.init(a.drop, a.N);
     float sum[8] = {};
@@ -130,11 +93,14 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
             if (a.act != MLP_ACT_NONE) {
                 float z[8];
                 load8((const T *)a.Z + r * a.ldz, c, a.N, z);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = activate_back(a.act, z[j], v[j]);
+                activate_back8(a.act, z, v);
             }
             if (a.drop.rng) drop8(st.bits(r, c), a.drop.threshold, a.drop.scale, v);
-            store8((T *)a.G + r * a.ldg, c, a.ldg, v);
+            if (c + 8 > a.N) {   // what pads a row is 0 (a'(0) dropped or not is not)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = c + j < a.N ? v[j] : 0.0f;
+            }
+            if (a.G) put8<T>(a.G + r * ldg + c, a.plane, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
         }
@@ -181,7 +147,6 @@ struct OnDevice {
     }
 };
 
-static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
 
 static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t max_rows) {
@@ -189,7 +154,7 @@ static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t 
            d_out <= LINEAR_MAX_WIDTH && max_rows >= 1 && max_rows <= MLP_MAX_BATCH;
 }
 
-// Workspace: g, then the partial column sums.
+// Workspace: the operands g, X and W, the partial column sums, the partial products.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -197,23 +162,43 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
         at += pad256(bytes);
         return p;
     };
-    c->ldg = (c->d_out + 7) / 8 * 8;
-    c->g = take((size_t)c->max_rows * c->ldg * dtype_bytes(c->dtype));
-    c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)c->d_out);
+    const size_t element = c->dtype == MLP_F32 ? 6 : 2;
+    const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
+    c->g = (uint16_t *)take(element * M * pad8(N));
+    c->x = (uint16_t *)take(element * M * pad8(K));
+    c->w = (uint16_t *)take(element * K * pad8(N));
+    c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
+    int64_t most = M * N > M * K ? M * N : M * K;
+    if (most < K * N) most = K * N;
+    c->part_floats = most < PART_FLOATS_MAX / 256 ? 256 * most : PART_FLOATS_MAX;
+    c->part = (float *)take(sizeof(float) * (size_t)c->part_floats);
     return at;
 }
 
+// The matrix [rows x cols] at P as an operand: as it is where its type and layout are an
+// operand's (rows close enough for 32-bit offsets within a tile), else packed at `room`.
 template <class T>
-static hipError_t product(const LinearCtx &c, const ProductArgs &a) {
-    const dim3 grid((unsigned)ceil_div(a.M, 64), (unsigned)ceil_div(a.N, 64));
-    hipLaunchKernelGGL(k_product<T>, grid, dim3(256), 0, c.stream, a);
+static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t rows, int64_t cols,
+                          uint16_t *room, Operand *o) {
+    if (rows <= 1) ld = pad8(cols);
+    if (sizeof(T) == 2 && ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < (1 << 22)) {
+        *o = Operand{(const uint16_t *)P, ld, 0};
+        return hipSuccess;
+    }
+    *o = Operand{room, pad8(cols), rows * pad8(cols)};
+    if (rows == 0) return hipSuccess;
+    const int64_t need = ceil_div(rows * (pad8(cols) / 8), 256);
+    hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)(need < 8192 ? need : 8192)), dim3(256), 0, c.stream,
+                       (const T *)P, ld, rows, cols, room, o->plane);
     return hipGetLastError();
 }
 
 template <class T>
 static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx, int64_t rows, const Epilogue &e) {
-    ProductArgs a{X, c.W, ldx, 1, c.d_out, 1, rows, c.d_out, c.d_in, e};
-    return product<T>(c, a);
+    Operand x, w;
+    if (hipError_t s = operand<T>(c, X, ldx, rows, c.d_in, c.x, &x)) return s;
+    if (hipError_t s = operand<T>(c, c.W, c.d_out, c.d_in, c.d_out, c.w, &w)) return s;
+    return launch_gemm(GEMM_NN, c.dtype, x, w, rows, c.d_out, c.d_in, e, c.part, c.part_floats, c.stream);
 }
 
 struct BackwardArgs {
@@ -227,8 +212,14 @@ struct BackwardArgs {
 template <class T>
 static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     const int64_t M = b.rows, N = c.d_out, K = c.d_in;
+    const bool products = M > 0 && (b.dX || b.dW);
+    // without activation and dropout g is dY, and dY itself the operand
+    const bool same = c.act == MLP_ACT_NONE && !b.drop.rng;
+    Operand g{c.g, pad8(N), M * pad8(N)};
+    if (products && same)
+        if (hipError_t e = operand<T>(c, b.dY, b.lddy, M, N, c.g, &g)) return e;
     int64_t chunks = 0;
-    if (M > 0) {
+    if (M > 0 && (b.db || (products && !same))) {
         GradArgs a;
         a.groups = 1;
         while (a.groups < 32 && a.groups * 8 < N) a.groups *= 2;
@@ -237,11 +228,11 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         chunks = ceil_div(M, a.chunk);
         a.Z = b.Z;
         a.dY = b.dY;
-        a.G = c.g;
+        a.G = products && !same ? c.g : nullptr;
         a.col = b.db ? c.col : nullptr;
         a.ldz = b.ldz;
         a.lddy = b.lddy;
-        a.ldg = c.ldg;
+        a.plane = g.plane;
         a.M = M;
         a.N = N;
         a.act = c.act;
@@ -257,14 +248,20 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     }
     Epilogue e{};
     if (b.dX && M > 0) {
+        Operand w;
+        if (hipError_t s = operand<T>(c, c.W, N, K, N, c.w, &w)) return s;
         e.Y = b.dX;
         e.ldy = b.lddx;
-        if (hipError_t s = product<T>(c, ProductArgs{c.g, c.W, c.ldg, 1, 1, N, M, K, N, e})) return s;
+        if (hipError_t s = launch_gemm(GEMM_NT, c.dtype, g, w, M, K, N, e, c.part, c.part_floats, c.stream))
+            return s;
     }
     if (b.dW) {
+        Operand x;
+        if (hipError_t s = operand<T>(c, b.X, b.ldx, M, K, c.x, &x)) return s;
         e.Y = b.dW;
         e.ldy = N;
-        if (hipError_t s = product<T>(c, ProductArgs{b.X, c.g, 1, b.ldx, c.ldg, 1, K, N, M, e})) return s;
+        if (hipError_t s = launch_gemm(GEMM_TN, c.dtype, x, g, K, N, M, e, c.part, c.part_floats, c.stream))
+            return s;
     }
     return hipSuccess;
 }

@@ -1,0 +1,362 @@
+// linear_gemm.hip -- the dense layer's matrix products on the matrix cores (gfx950):
+// bf16 and fp16 operands as they are, fp32 ones as three bf16 parts (bf16x3.h: six part
+// products each, the leading one and the five smaller ones in sums of their own).
+//
+// A workgroup computes a TM x TN tile of C; its K loop runs over chunks of BK staged in
+// LDS, two buffers, each chunk's loads issued straight to LDS while the chunk before it
+// is on the matrix cores: one barrier a chunk. The products are v_mfma_f32_32x32x16 with
+// B as the first operand, so that four of a lane's results in a row lie along a row of C.
+//
+// An operand whose k is contiguous lies in LDS as [x][k], read in 16-byte pieces; one
+// whose x is contiguous as [k][x], read by ds_read_b64_tr_b16, which hands each lane
+// four consecutive k of its x. The 16-byte pieces of a row are permuted by the row's
+// number, by way of the addresses they are loaded from, to spread reads over the banks.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "linear_internal.h"
+
+namespace mlp {
+
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+
+template <class T>
+__device__ __forceinline__ f16v mma(u4v a, u4v b, f16v c);
+template <>
+__device__ __forceinline__ f16v mma<bf16>(u4v a, u4v b, f16v c) {
+    return mfma_bf16_32(a, b, c);
+}
+template <>
+__device__ __forceinline__ f16v mma<f16>(u4v a, u4v b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8v, a), __builtin_bit_cast(h8v, b), c, 0, 0, 0);
+}
+
+// Where lanes with nothing to load (past the end of K) load from.
+static __device__ __attribute__((aligned(16))) uint32_t g_zeros[4] = {0, 0, 0, 0};
+
+__device__ __forceinline__ void to_lds(const void *g, void *l) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(uintptr_t)g,
+                                     (__attribute__((address_space(3))) uint32_t *)(uintptr_t)l, 16, 0, 0);
+}
+
+// One operand's chunks: TX values of x by BK of k, NP parts, moved by NT threads.
+// XC: x is contiguous in memory (P[k][x]), else k is (P[x][k]).
+template <bool XC, int TX, int BK, int NP, int NT>
+struct Tile {
+    static constexpr int K = BK;
+    static constexpr int ROW = XC ? TX : BK;              // elements of an LDS row
+    static constexpr int PIECES = TX * BK / 8;            // 16-byte pieces of a part
+    static constexpr int LOADS = PIECES / NT;
+    static constexpr int ELEMS = NP * TX * BK;
+    static_assert(PIECES % NT == 0, "every thread moves the same number of pieces");
+
+    const char *base;        // the current chunk's corner, uniform
+    uint32_t off[LOADS];     // bytes from it
+    int64_t step, plane;     // bytes to the next chunk, to the next part
+
+    // the permutation of a row's pieces
+    static __device__ __forceinline__ int swz(int row) {
+        if constexpr (XC) return 2 * (row & 3) & (ROW / 8 - 1);
+        else if constexpr (BK == 64) return row & 7;
+        else return (row >> 1) & 3;
+    }
+    __device__ __forceinline__ void init(const Operand &o, int64_t x0, int64_t xlim, int64_t k0) {
+        base = (const char *)(o.p + (XC ? k0 * o.ld + x0 : x0 * o.ld + k0));
+        step = 2 * (XC ? BK * o.ld : (int64_t)BK);
+        plane = 2 * o.plane;
+        // what lies past the matrix in x gives sums that are not kept: any value will
+        // do, the last row or piece of the matrix is read in its place
+        const int last = (int)(xlim - x0 < TX ? xlim - x0 : TX) - 1;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int q = i * NT + threadIdx.x, row = q / (ROW / 8), c = (q % (ROW / 8)) ^ swz(row);
+            const int at = XC ? (c < last / 8 ? c : last / 8) : c, r = XC ? row : (row < last ? row : last);
+            off[i] = 2u * (uint32_t)(r * (uint32_t)o.ld + 8u * at);
+        }
+    }
+    // the chunk at base to the LDS tile S, base to the next one; TAIL: only k < left
+    template <bool TAIL>
+    __device__ __forceinline__ void load(uint16_t *S, int left) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                uint16_t *d = S + p * (TX * BK) + 8 * (i * NT + (threadIdx.x & ~63u));
+                const char *g = base + p * plane + off[i];
+                if constexpr (TAIL) {
+                    const int q = i * NT + threadIdx.x, row = q / (ROW / 8);
+                    const int k = XC ? row : 8 * ((q % (ROW / 8)) ^ swz(row));
+                    if (k >= left) g = (const char *)g_zeros;
+                }
+                to_lds(g, d);
+            }
+        base += step;
+    }
+    // k in [16 kk, 16 kk + 16) of x in [x, x + 32), as an MFMA operand: lane l has x + l
+    // % 32 and the eight k of its half l / 32
+    static __device__ __forceinline__ u4v frag(const uint16_t *S, int x, int kk, int p) {
+        const int l = threadIdx.x & 63;
+        S += p * (TX * BK);
+        if constexpr (XC) {
+            // of 16 lanes, four read four x of one of four consecutive k each
+            const int k = 16 * kk + 8 * (l >> 5) + ((l >> 2) & 3), xx = x + 16 * ((l >> 4) & 1) + 4 * (l & 3);
+            const int at = (((xx >> 3) ^ swz(k)) << 3) | (xx & 7);
+            typedef __attribute__((address_space(3))) s4v lds4;
+            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)(S + k * ROW + at));
+            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)(S + (k + 4) * ROW + at));
+            const u2v a = __builtin_bit_cast(u2v, lo), b = __builtin_bit_cast(u2v, hi);
+            return u4v{a[0], a[1], b[0], b[1]};
+        } else {
+            const int row = x + (l & 31), c = 2 * kk + (l >> 5);
+            return *reinterpret_cast<const u4v *>(S + row * ROW + ((c ^ swz(row)) << 3));
+        }
+    }
+};
+
+// A wave's LDS writes before its lanes' reads of one another's (and the reverse).
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int NP, int NJ, int MI>
+struct Sums {
+    f16v acc[NJ][MI], lo[NP == 3 ? NJ : 1][NP == 3 ? MI : 1];
+};
+
+// The next chunk of both operands to LDS; left: its k (BK, but for the last chunk)
+template <class TA, class TB>
+__device__ __forceinline__ void load_chunk(TA &a, TB &b, uint16_t *An, uint16_t *Bn, int left) {
+    if (left == TA::K) {
+        a.template load<false>(An, left);
+        b.template load<false>(Bn, left);
+    } else {
+        a.template load<true>(An, left);
+        b.template load<true>(Bn, left);
+    }
+}
+
+// One chunk on the matrix cores (Ac, Bc) while the next one is loaded (An, Bn). The
+// buffers are restrict parameters of a function of its own: only so does the compiler
+// know that the loads to LDS in flight do not write what is read here, and does not wait
+// for them first.
+template <class T, int NP, int NJ, int MI, int BK, class TA, class TB>
+__device__ __forceinline__ void chunk_step(TA &a, TB &b, Sums<NP, NJ, MI> &sum, uint16_t *__restrict__ An,
+                                           uint16_t *__restrict__ Bn, const uint16_t *__restrict__ Ac,
+                                           const uint16_t *__restrict__ Bc, bool more, int left, int wm, int wn) {
+    if (more) load_chunk(a, b, An, Bn, left);
+#pragma unroll
+    for (int kk = 0; kk < BK / 16; ++kk) {
+        u4v af[MI][NP], bf[NJ][NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) bf[j][p] = TB::frag(Bc, wn + 32 * j, kk, p);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) af[i][p] = TA::frag(Ac, wm + 32 * i, kk, p);
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                if constexpr (NP == 3) {
+                    constexpr int PA[5] = {2, 1, 0, 1, 0}, PB[5] = {0, 1, 2, 0, 1};
+#pragma unroll
+                    for (int p = 0; p < 5; ++p)
+                        sum.lo[j][i] = mfma_bf16_32(bf[j][PB[p]], af[i][PA[p]], sum.lo[j][i]);
+                    sum.acc[j][i] = mfma_bf16_32(bf[j][0], af[i][0], sum.acc[j][i]);
+                } else {
+                    sum.acc[j][i] = mma<T>(bf[j][0], af[i][0], sum.acc[j][i]);
+                }
+            }
+    }
+}
+
+// TM x TN outputs, WM x WN waves, each TM / WM x TN / WN outputs as 32 x 32 MFMA tiles.
+// T: the type of C; NP = 3: fp32 operands in parts.
+template <class T, int OP, int TM, int TN, int BK, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, NT = 64 * WM * WN;
+    constexpr int MI = TM / WM / 32, NJ = TN / WN / 32;
+    typedef Tile<OP == GEMM_TN, TM, BK, NP, NT> TA;
+    typedef Tile<OP != GEMM_NT, TN, BK, NP, NT> TB;
+    constexpr int WTN = TN / WN, CS = WTN + 4;   // a wave's columns; row stride of its results in LDS
+    static_assert(WM * WN * 32 * CS * 4 <= 4 * (TA::ELEMS + TB::ELEMS), "the results fit where the chunks were");
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * (TA::ELEMS + TB::ELEMS)];   // two chunks of A and B
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
+
+    // Workgroups go round the eight XCDs in turn: each XCD takes consecutive tiles, eight
+    // rows of tiles at a time down a column, so that its L2 keeps what they share.
+    const int tiles = g.tiles_m * g.tiles_n;
+    int id = blockIdx.x;
+    const int split = id / tiles;
+    id -= split * tiles;
+    {
+        const int per = tiles / 8, extra = tiles % 8, x = id % 8;
+        id = x * per + (x < extra ? x : extra) + id / 8;
+    }
+    const int band = 8 * g.tiles_n, b0 = id / band * 8;
+    const int bh = g.tiles_m - b0 < 8 ? g.tiles_m - b0 : 8;
+    const int in = id % band;
+    const int64_t m0 = (int64_t)(b0 + in % bh) * TM, n0 = (int64_t)(in / bh) * TN;
+
+    const int64_t kb = (int64_t)split * g.kc, ke = kb + g.kc < g.K ? kb + g.kc : g.K;
+    const int nk = (int)((ke - kb + BK - 1) / BK);
+    const int tail = (int)(ke - kb) - (nk - 1) * BK;   // k of the last chunk
+
+    Sums<NP, NJ, MI> sum;
+    auto &acc = sum.acc;
+    auto &lo = sum.lo;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                acc[j][i][v] = 0.f;
+                if constexpr (NP == 3) lo[j][i][v] = 0.f;
+            }
+
+    if (nk > 0) {
+        TA a;
+        TB b;
+        a.init(g.A, m0, g.M, kb);
+        b.init(g.B, n0, g.N, kb);
+        // chunk c: the barrier ends every wave's loads of it and its reads of chunk
+        // c - 1, whose buffer chunk c + 1 then takes
+        load_chunk(a, b, lds, lds + TA::ELEMS, nk > 1 ? BK : tail);
+        uint32_t now = 0, next = TA::ELEMS + TB::ELEMS;
+        for (int c = 0; c < nk; ++c) {
+            __syncthreads();
+            chunk_step<T, NP, NJ, MI, BK>(a, b, sum, lds + next, lds + next + TA::ELEMS, lds + now,
+                                          lds + now + TA::ELEMS, c + 1 < nk, c + 2 < nk ? BK : tail, wm, wn);
+            const uint32_t t = now;
+            now = next;
+            next = t;
+        }
+    }
+
+    // The results, 32 rows of a wave at a time, through LDS: a lane's registers hold four
+    // columns here and there of one row, memory is read and written along the rows.
+    __syncthreads();
+    float *C = reinterpret_cast<float *>(lds) + wave * 32 * CS;
+    DropState st;
+    if (g.e.drop.rng) st.init(g.e.drop, g.N);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    v[r] = acc[j][i][4 * q + r];
+                    if constexpr (NP == 3) v[r] += lo[j][i][4 * q + r];
+                }
+                *reinterpret_cast<f4 *>(C + (lane & 31) * CS + 32 * j + 8 * q + 4 * (lane >> 5)) = v;
+            }
+        wave_sync();
+        constexpr int GROUPS = WTN / 8, ROWS = 64 / GROUPS;
+#pragma unroll 1
+        for (int r = lane / GROUPS; r < 32; r += ROWS) {
+            const int64_t m = m0 + wm + 32 * i + r, n = n0 + wn + 8 * (lane % GROUPS);
+            if (m >= g.M || n >= g.N) continue;
+            float v[8];
+            const f4 *c = reinterpret_cast<const f4 *>(C + r * CS + 8 * (lane % GROUPS));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = c[k / 4][k % 4];
+            if (g.splits > 1) store8(g.part + ((int64_t)split * g.M + m) * g.N, n, g.N, v);
+            else finish8<T>(g.e, st, m, n, g.N, v);
+        }
+        wave_sync();
+    }
+}
+
+// The splits' sums, in order, through the epilogue.
+template <class T>
+__global__ __launch_bounds__(256) void k_gemm_join(const GemmArgs g) {
+    DropState st;
+    if (g.e.drop.rng) st.init(g.e.drop, g.N);
+    const int64_t blocks = (g.N + 7) / 8, total = g.M * blocks, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const int64_t m = i / blocks, n = (i - m * blocks) * 8;
+        float v[8];
+        load8(g.part + m * g.N, n, g.N, v);
+        for (int s = 1; s < g.splits; ++s) {
+            float w[8];
+            load8(g.part + (s * g.M + m) * g.N, n, g.N, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w[j];
+        }
+        finish8<T>(g.e, st, m, n, g.N, v);
+    }
+}
+
+template <class T, int OP, int TM, int TN, int BK, int WM, int WN>
+static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream) {
+    constexpr int64_t CUS = 256;
+    g.tiles_m = (int)ceil_div(g.M, TM);
+    g.tiles_n = (int)ceil_div(g.N, TN);
+    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n, chunks = ceil_div(g.K, BK);
+    int64_t splits = tiles < CUS ? CUS / tiles : 1;
+    if (splits > chunks / 4) splits = chunks / 4;
+    if (splits > part_floats / (g.M * g.N)) splits = part_floats / (g.M * g.N);
+    if (splits < 1) splits = 1;
+    g.kc = ceil_div(chunks, splits) * BK;
+    g.splits = g.K > 0 ? (int)ceil_div(g.K, g.kc) : 1;
+    hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, WM, WN>), dim3((unsigned)(tiles * g.splits)),
+                       dim3(64 * WM * WN), 0, stream, g);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (g.splits > 1) {
+        const int64_t need = ceil_div(g.M * ceil_div(g.N, 8), 256);
+        hipLaunchKernelGGL(k_gemm_join<T>, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, stream, g);
+    }
+    return hipGetLastError();
+}
+
+template <class T, int OP>
+static hipError_t gemm_op(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
+    const int64_t big = ceil_div(g.M, 256) * ceil_div(g.N, 256), mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
+    if constexpr (sizeof(T) == 2) {
+        if (big >= 200) return gemm_tiles<T, OP, 256, 256, 64, 2, 4>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 64, 2, 2>(g, part_floats, stream);
+        return gemm_tiles<T, OP, 64, 64, 64, 2, 2>(g, part_floats, stream);
+    } else {
+        if (mid >= 400) return gemm_tiles<T, OP, 256, 128, 32, 4, 2>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 2, 2>(g, part_floats, stream);
+        return gemm_tiles<T, OP, 64, 64, 32, 2, 2>(g, part_floats, stream);
+    }
+}
+
+template <class T>
+static hipError_t gemm_type(int op, const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
+    switch (op) {
+    case GEMM_NN: return gemm_op<T, GEMM_NN>(g, part_floats, stream);
+    case GEMM_NT: return gemm_op<T, GEMM_NT>(g, part_floats, stream);
+    default: return gemm_op<T, GEMM_TN>(g, part_floats, stream);
+    }
+}
+
+hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N,
+                       int64_t K, const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream) {
+    GemmArgs g{};
+    g.A = A;
+    g.B = B;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.part = part;
+    g.e = e;
+    switch (dtype) {
+    case MLP_F32: return gemm_type<float>(op, g, part_floats, stream);
+    case MLP_BF16: return gemm_type<bf16>(op, g, part_floats, stream);
+    default: return gemm_type<f16>(op, g, part_floats, stream);
+    }
+}
+
+}  // namespace mlp

@@ -1,0 +1,75 @@
+// linear_internal.h -- shared declarations of the dense layer: its epilogue and the
+// matrix product on the matrix cores (linear.hip, linear_gemm.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "layer.h"
+
+namespace mlp {
+
+// What becomes of the fp32 sums of a matrix product: Y = R + dropout(a(sum + bias)),
+// Z = sum + bias; everything but Y may be missing.
+struct Epilogue {
+    const void *bias, *R;
+    void *Z, *Y;
+    int64_t ldr, ldz, ldy;
+    int act;
+    Drop drop;
+};
+
+// The sums of columns [c, c + 8) of row r, c a multiple of 8; columns from n on are not
+// touched.
+template <class T>
+__device__ __forceinline__ void finish8(const Epilogue &e, const DropState &st, int64_t r, int64_t c,
+                                        int64_t n, float (&v)[8]) {
+    if (e.bias) {
+        float b[8];
+        load8((const T *)e.bias, c, n, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+    if (e.Z) store8((T *)e.Z + r * e.ldz, c, n, v);
+    activate8(e.act, v);
+    if (e.drop.rng) drop8(st.bits(r, c), e.drop.threshold, e.drop.scale, v);
+    if (e.R) {
+        float q[8];
+        load8((const T *)e.R + r * e.ldr, c, n, q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += q[j];
+    }
+    store8((T *)e.Y + r * e.ldy, c, n, v);
+}
+
+// An operand of a product on the matrix cores, as 16-bit values: rows of `ld` elements,
+// 16-byte aligned, ld and the length of a row multiples of 8 (what pads a row is zero).
+// fp32 operands are three such matrices of bf16 parts (bf16x3.h), `plane` elements apart.
+struct Operand {
+    const uint16_t *p;
+    int64_t ld, plane;
+};
+
+// C[m][n] = sum_k a(m, k) b(k, n) for m < M, n < N, k < K. The products there are:
+// NN: a(m, k) = A[m][k], b(k, n) = B[k][n]; NT: b(k, n) = B[n][k]; TN: a(m, k) = A[k][m],
+// b(k, n) = B[k][n].
+enum { GEMM_NN = 0, GEMM_NT = 1, GEMM_TN = 2 };
+
+struct GemmArgs {
+    Operand A, B;
+    int64_t M, N, K;
+    int64_t kc;              // depth of a split (a multiple of the chunk)
+    int tiles_m, tiles_n, splits;
+    float *part;             // splits > 1: [splits][M][N] fp32 sums
+    Epilogue e;
+};
+
+// C (through e) of type dtype; part: room for part_floats partial sums. One or two
+// launches on `stream`.
+hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N,
+                       int64_t K, const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream);
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace mlp
