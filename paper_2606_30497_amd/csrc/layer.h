@@ -122,13 +122,34 @@ __device__ __forceinline__ void drop8(u4v bits, uint32_t threshold, float scale,
 
 // ---- activations ------------------------------------------------------------------------
 
-// 1 / (1 + exp(-t))
-__device__ __forceinline__ float sigmoid(float t) { return 1.0f / (1.0f + expf(-t)); }
+// 1 / (1 + exp(-t)), by the hardware's exponential and reciprocal (a few 2^-24 of its
+// value, and |t| 2^-24 from the rounding of the exponent)
+__device__ __forceinline__ float sigmoid(float t) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504f));
+}
 
 constexpr float GELU_C = 1.5957691216057308f;   // 2 sqrt(2 / pi): z / (1 + exp(-C (z + 0.044715 z^3)))
 constexpr float GELU_A = 0.044715f;
 
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.0f + erff(z * 0.70710678f)); }
+// The normal distribution function: Phi(-x) = e^(-x^2 / 2) F(x) for x >= 0, where F, with
+// t = 1 / (1 + 0.31 x), is t times a polynomial in t (degree 7, fitted to F = erfcx(x /
+// sqrt 2) / 2 for the least largest relative error, 1.6e-7; in fp32 Phi is within 2.2e-7
+// of exact). A third of the instructions of 1 + erf, and e^(-z^2 / 2) (in `bell`) is the
+// derivative's. For GELU of a 256 x 256 tile that is the larger part of its epilogue.
+__device__ __forceinline__ float normal_cdf(float z, float &bell) {
+    const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.31f, x, 1.0f));
+    float p = 0.035841804f;
+    p = fmaf(p, t, -0.14160487f);
+    p = fmaf(p, t, 0.15506828f);
+    p = fmaf(p, t, -0.014903724f);
+    p = fmaf(p, t, 0.11011028f);
+    p = fmaf(p, t, 0.10777105f);
+    p = fmaf(p, t, 0.12406035f);
+    p = fmaf(p, t, 0.12365691f);
+    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    const float q = p * t * bell;
+    return z < 0.0f ? q : 1.0f - q;
+}
 
 // v <- a(v)
 __device__ __forceinline__ void activate8(int act, float (&v)[8]) {
@@ -139,7 +160,10 @@ __device__ __forceinline__ void activate8(int act, float (&v)[8]) {
         break;
     case MLP_ACT_GELU:
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= normal_cdf(v[j]);
+        for (int j = 0; j < 8; ++j) {
+            float bell;
+            v[j] *= normal_cdf(v[j], bell);
+        }
         break;
     case MLP_ACT_GELU_TANH:
 #pragma unroll
@@ -161,7 +185,11 @@ __device__ __forceinline__ void activate_back8(int act, const float (&z)[8], flo
         break;
     case MLP_ACT_GELU:   // Phi(z) + z phi(z)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= normal_cdf(z[j]) + z[j] * 0.39894228f * expf(-0.5f * z[j] * z[j]);
+        for (int j = 0; j < 8; ++j) {
+            float bell;
+            const float cdf = normal_cdf(z[j], bell);
+            v[j] *= cdf + z[j] * 0.39894228f * bell;
+        }
         break;
     case MLP_ACT_GELU_TANH:
 #pragma unroll

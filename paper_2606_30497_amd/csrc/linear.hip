@@ -123,14 +123,24 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
     }
 }
 
-// db[n] = sum over the chunks, in order
+// db[n] = the sum of the chunks' column sums: 32 columns a workgroup, each by eight
+// threads that take every eighth chunk, summed in order.
 template <class T>
 __global__ __launch_bounds__(256) void k_column_sums(const float *col, int64_t chunks, int64_t N, T *db) {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
+    __shared__ float part[8][33];
+    const int t = threadIdx.x & 31, q = threadIdx.x >> 5;
+    const int64_t n = (int64_t)blockIdx.x * 32 + t;
     float s = 0.0f;
-    for (int64_t i = 0; i < chunks; ++i) s += col[i * N + n];
-    db[n] = (T)s;
+    if (n < N)
+#pragma unroll 4
+        for (int64_t i = q; i < chunks; i += 8) s += col[i * N + n];
+    part[q][t] = s;
+    __syncthreads();
+    if (q == 0 && n < N) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += part[i][t];
+        db[n] = (T)s;
+    }
 }
 
 // The context's device, current for the length of a call.
@@ -224,7 +234,9 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.groups = 1;
         while (a.groups < 32 && a.groups * 8 < N) a.groups *= 2;
         const int64_t step = 256 / a.groups;
-        a.chunk = ceil_div(ceil_div(M, COL_CHUNKS), step) * step;
+        // about four workgroups a compute unit
+        const int64_t want = ceil_div(1024, ceil_div(N, 8 * a.groups));
+        a.chunk = ceil_div(ceil_div(M, want < COL_CHUNKS ? want : COL_CHUNKS), step) * step;
         chunks = ceil_div(M, a.chunk);
         a.Z = b.Z;
         a.dY = b.dY;
@@ -242,7 +254,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (b.db) {
-        hipLaunchKernelGGL(k_column_sums<T>, dim3((unsigned)ceil_div(N, 256)), dim3(256), 0, c.stream, c.col,
+        hipLaunchKernelGGL(k_column_sums<T>, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, c.stream, c.col,
                            chunks, N, (T *)b.db);
         if (hipError_t e = hipGetLastError()) return e;
     }

@@ -3,8 +3,8 @@
 // products each, the leading one and the five smaller ones in sums of their own).
 //
 // A workgroup computes a TM x TN tile of C; its K loop runs over chunks of BK staged in
-// LDS, two buffers, each chunk's loads issued straight to LDS while the chunk before it
-// is on the matrix cores: one barrier a chunk. The products are v_mfma_f32_32x32x16 with
+// LDS, in three to five stages: a chunk's loads go straight to LDS while the chunks before
+// it are on the matrix cores, one barrier a chunk. The products are v_mfma_f32_32x32x16 with
 // B as the first operand, so that four of a lane's results in a row lie along a row of C.
 //
 // An operand whose k is contiguous lies in LDS as [x][k], read in 16-byte pieces; one
@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "linear_internal.h"
 
@@ -45,10 +47,11 @@ __device__ __forceinline__ void to_lds(const void *g, void *l) {
 // XC: x is contiguous in memory (P[k][x]), else k is (P[x][k]).
 template <bool XC, int TX, int BK, int NP, int NT>
 struct Tile {
-    static constexpr int K = BK;
+    static constexpr int K = BK, PARTS = NP;
     static constexpr int ROW = XC ? TX : BK;              // elements of an LDS row
     static constexpr int PIECES = TX * BK / 8;            // 16-byte pieces of a part
     static constexpr int LOADS = PIECES / NT;
+    static constexpr int READS = XC ? 2 : 1;              // LDS reads of a fragment
     static constexpr int ELEMS = NP * TX * BK;
     static_assert(PIECES % NT == 0, "every thread moves the same number of pieces");
 
@@ -56,11 +59,12 @@ struct Tile {
     uint32_t off[LOADS];     // bytes from it
     int64_t step, plane;     // bytes to the next chunk, to the next part
 
-    // the permutation of a row's pieces
+    // The permutation of a row's pieces: LDS has 64 banks of 4 bytes, and the 16 rows
+    // that a 16-byte read meets at one piece, or the four rows that a transposing read
+    // meets at two pieces each, fall on all of them.
     static __device__ __forceinline__ int swz(int row) {
-        if constexpr (XC) return 2 * (row & 3) & (ROW / 8 - 1);
-        else if constexpr (BK == 64) return row & 7;
-        else return (row >> 1) & 3;
+        if constexpr (XC) return TX >= 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+        else return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
     }
     __device__ __forceinline__ void init(const Operand &o, int64_t x0, int64_t xlim, int64_t k0) {
         base = (const char *)(o.p + (XC ? k0 * o.ld + x0 : x0 * o.ld + k0));
@@ -76,23 +80,19 @@ struct Tile {
             off[i] = 2u * (uint32_t)(r * (uint32_t)o.ld + 8u * at);
         }
     }
-    // the chunk at base to the LDS tile S, base to the next one; TAIL: only k < left
+    // one of the NP * LOADS loads of the chunk at base to the LDS tile S; TAIL: only k <
+    // left is there, zeros take the place of the rest
     template <bool TAIL>
-    __device__ __forceinline__ void load(uint16_t *S, int left) {
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                uint16_t *d = S + p * (TX * BK) + 8 * (i * NT + (threadIdx.x & ~63u));
-                const char *g = base + p * plane + off[i];
-                if constexpr (TAIL) {
-                    const int q = i * NT + threadIdx.x, row = q / (ROW / 8);
-                    const int k = XC ? row : 8 * ((q % (ROW / 8)) ^ swz(row));
-                    if (k >= left) g = (const char *)g_zeros;
-                }
-                to_lds(g, d);
-            }
-        base += step;
+    __device__ __forceinline__ void load(uint16_t *S, int n, int left) const {
+        const int p = n / LOADS, i = n % LOADS;
+        uint16_t *d = S + p * (TX * BK) + 8 * (i * NT + (threadIdx.x & ~63u));
+        const char *g = base + p * plane + off[i];
+        if constexpr (TAIL) {
+            const int q = i * NT + threadIdx.x, row = q / (ROW / 8);
+            const int k = XC ? row : 8 * ((q % (ROW / 8)) ^ swz(row));
+            if (k >= left) g = (const char *)g_zeros;
+        }
+        to_lds(g, d);
     }
     // k in [16 kk, 16 kk + 16) of x in [x, x + 32), as an MFMA operand: lane l has x + l
     // % 32 and the eight k of its half l / 32
@@ -122,70 +122,124 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// f(0), f(1), ... f(N - 1), each with its number as a constant
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        unrolled<N, I + 1>(f);
+    }
+}
+
 template <int NP, int NJ, int MI>
 struct Sums {
     f16v acc[NJ][MI], lo[NP == 3 ? NJ : 1][NP == 3 ? MI : 1];
 };
 
-// The next chunk of both operands to LDS; left: its k (BK, but for the last chunk)
-template <class TA, class TB>
-__device__ __forceinline__ void load_chunk(TA &a, TB &b, uint16_t *An, uint16_t *Bn, int left) {
-    if (left == TA::K) {
-        a.template load<false>(An, left);
-        b.template load<false>(Bn, left);
-    } else {
-        a.template load<true>(An, left);
-        b.template load<true>(Bn, left);
+// Loads [n0, n1) of a chunk of both operands (the A tile's, then the B tile's).
+template <bool TAIL, int N0, int N1, class TA, class TB>
+__device__ __forceinline__ void load_some(const TA &a, const TB &b, uint16_t *An, uint16_t *Bn, int left) {
+    constexpr int NA = TA::PARTS * TA::LOADS;
+#pragma unroll
+    for (int n = N0; n < N1; ++n) {
+        if (n < NA) a.template load<TAIL>(An, n, left);
+        else b.template load<TAIL>(Bn, n - NA, left);
     }
 }
 
-// One chunk on the matrix cores (Ac, Bc) while the next one is loaded (An, Bn). The
-// buffers are restrict parameters of a function of its own: only so does the compiler
-// know that the loads to LDS in flight do not write what is read here, and does not wait
-// for them first.
-template <class T, int NP, int NJ, int MI, int BK, class TA, class TB>
-__device__ __forceinline__ void chunk_step(TA &a, TB &b, Sums<NP, NJ, MI> &sum, uint16_t *__restrict__ An,
-                                           uint16_t *__restrict__ Bn, const uint16_t *__restrict__ Ac,
-                                           const uint16_t *__restrict__ Bc, bool more, int left, int wm, int wn) {
-    if (more) load_chunk(a, b, An, Bn, left);
-#pragma unroll
-    for (int kk = 0; kk < BK / 16; ++kk) {
-        u4v af[MI][NP], bf[NJ][NP];
+// Every wave has loaded its pieces but for the last N loads it issued, and is done with
+// what it read before.
+template <int N>
+__device__ __forceinline__ void loaded_all_but() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The operands of 16 k for a wave's products.
+template <int NP, int NJ, int MI>
+struct Frags {
+    u4v a[MI][NP], b[NJ][NP];
+    template <class TA, class TB>
+    __device__ __forceinline__ void fetch(const uint16_t *A, const uint16_t *B, int wm, int wn, int kk) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) bf[j][p] = TB::frag(Bc, wn + 32 * j, kk, p);
+            for (int j = 0; j < NJ; ++j) b[j][p] = TB::frag(B, wn + 32 * j, kk, p);
 #pragma unroll
-            for (int i = 0; i < MI; ++i) af[i][p] = TA::frag(Ac, wm + 32 * i, kk, p);
+            for (int i = 0; i < MI; ++i) a[i][p] = TA::frag(A, wm + 32 * i, kk, p);
+        }
+    }
+    // the products of row j of the wave's tiles
+    template <class T>
+    __device__ __forceinline__ void multiply(Sums<NP, NJ, MI> &s, int j) const {
+        if constexpr (NP == 3) {
+            constexpr int PA[5] = {2, 1, 0, 1, 0}, PB[5] = {0, 1, 2, 0, 1};
+#pragma unroll
+            for (int p = 0; p < 5; ++p)
+#pragma unroll
+                for (int i = 0; i < MI; ++i) s.lo[j][i] = mfma_bf16_32(b[j][PB[p]], a[i][PA[p]], s.lo[j][i]);
         }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                if constexpr (NP == 3) {
-                    constexpr int PA[5] = {2, 1, 0, 1, 0}, PB[5] = {0, 1, 2, 0, 1};
-#pragma unroll
-                    for (int p = 0; p < 5; ++p)
-                        sum.lo[j][i] = mfma_bf16_32(bf[j][PB[p]], af[i][PA[p]], sum.lo[j][i]);
-                    sum.acc[j][i] = mfma_bf16_32(bf[j][0], af[i][0], sum.acc[j][i]);
-                } else {
-                    sum.acc[j][i] = mma<T>(bf[j][0], af[i][0], sum.acc[j][i]);
-                }
-            }
+        for (int i = 0; i < MI; ++i) {
+            if constexpr (NP == 3) s.acc[j][i] = mfma_bf16_32(b[j][0], a[i][0], s.acc[j][i]);
+            else s.acc[j][i] = mma<T>(b[j][0], a[i][0], s.acc[j][i]);
+        }
     }
+};
+
+// One chunk (at Ac, Bc) on the matrix cores, while a later one is loaded (to An, Bn): each
+// 16 k are read from LDS while the 16 before are multiplied; f[0] holds the chunk's first.
+// AHEAD (three stages or more): the first of the chunk that follows (at Af, Bf) are read
+// too. The buffers are restrict parameters of a function of its own: only so does the
+// compiler know that the loads to LDS in flight do not write what is read here, and does
+// not wait for them first. The loads are spread over the products, since a wave that
+// issues them in a row waits for the address unit, which takes 16 cycles for each (TN of
+// 8,192 x 8,192 x 8,192 in bf16 1,218 us in a row, 870 us spread); with two stages over
+// the first three eighths of the chunk (NT 875 us; over five eighths 911, over all 934).
+template <bool TAIL, bool AHEAD, class T, int NP, int NJ, int MI, class TA, class TB>
+__device__ __forceinline__ void chunk_step(const TA &a, const TB &b, Sums<NP, NJ, MI> &sum,
+                                           Frags<NP, NJ, MI> (&f)[2], uint16_t *__restrict__ An,
+                                           uint16_t *__restrict__ Bn, const uint16_t *__restrict__ Ac,
+                                           const uint16_t *__restrict__ Bc, const uint16_t *__restrict__ Af,
+                                           const uint16_t *__restrict__ Bf, int left, int wm, int wn) {
+    constexpr int KK = TA::K / 16, SLOTS = AHEAD ? KK * NJ : 3 * KK * NJ / 8;
+    constexpr int ALL = TA::PARTS * TA::LOADS + TB::PARTS * TB::LOADS;
+    constexpr int MFMAS = MI * (NP == 3 ? 6 : 1);
+    constexpr int EACH = 2;   // LDS reads after a product
+    static_assert(KK % 2 == 0, "the next chunk's first operands go to f[0]");
+    unrolled<KK>([&](auto kkc) __attribute__((always_inline)) {
+        constexpr int kk = decltype(kkc)::value;
+        if constexpr (kk + 1 < KK) f[(kk + 1) & 1].template fetch<TA, TB>(Ac, Bc, wm, wn, kk + 1);
+        else if constexpr (AHEAD) f[0].template fetch<TA, TB>(Af, Bf, wm, wn, 0);
+        unrolled<NJ>([&](auto jc) __attribute__((always_inline)) {
+            constexpr int j = decltype(jc)::value, slot = kk * NJ + j;
+            if constexpr (slot < SLOTS)
+                load_some<TAIL, ALL * slot / SLOTS, ALL *(slot + 1) / SLOTS>(a, b, An, Bn, left);
+            f[kk & 1].template multiply<T>(sum, j);
+#pragma unroll
+            for (int n = 0; n < MFMAS; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    });
 }
 
 // TM x TN outputs, WM x WN waves, each TM / WM x TN / WN outputs as 32 x 32 MFMA tiles.
-// T: the type of C; NP = 3: fp32 operands in parts.
-template <class T, int OP, int TM, int TN, int BK, int WM, int WN>
+// T: the type of C; NP = 3: fp32 operands in parts. S: LDS stages, each a chunk of both
+// operands.
+template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, NT = 64 * WM * WN;
     constexpr int MI = TM / WM / 32, NJ = TN / WN / 32;
     typedef Tile<OP == GEMM_TN, TM, BK, NP, NT> TA;
     typedef Tile<OP != GEMM_NT, TN, BK, NP, NT> TB;
     constexpr int WTN = TN / WN, CS = WTN + 4;   // a wave's columns; row stride of its results in LDS
-    static_assert(WM * WN * 32 * CS * 4 <= 4 * (TA::ELEMS + TB::ELEMS), "the results fit where the chunks were");
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * (TA::ELEMS + TB::ELEMS)];   // two chunks of A and B
+    static_assert(WM * WN * 32 * CS * 4 <= 2 * S * (TA::ELEMS + TB::ELEMS), "the results fit where the chunks were");
+    constexpr int STAGE = TA::ELEMS + TB::ELEMS;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S * STAGE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
 
@@ -206,8 +260,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
 
     const int64_t kb = (int64_t)split * g.kc, ke = kb + g.kc < g.K ? kb + g.kc : g.K;
     const int nk = (int)((ke - kb + BK - 1) / BK);
-    const int tail = (int)(ke - kb) - (nk - 1) * BK;   // k of the last chunk
-
     Sums<NP, NJ, MI> sum;
     auto &acc = sum.acc;
     auto &lo = sum.lo;
@@ -226,18 +278,44 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
         TB b;
         a.init(g.A, m0, g.M, kb);
         b.init(g.B, n0, g.N, kb);
-        // chunk c: the barrier ends every wave's loads of it and its reads of chunk
-        // c - 1, whose buffer chunk c + 1 then takes
-        load_chunk(a, b, lds, lds + TA::ELEMS, nk > 1 ? BK : tail);
-        uint32_t now = 0, next = TA::ELEMS + TB::ELEMS;
-        for (int c = 0; c < nk; ++c) {
-            __syncthreads();
-            chunk_step<T, NP, NJ, MI, BK>(a, b, sum, lds + next, lds + next + TA::ELEMS, lds + now,
-                                          lds + now + TA::ELEMS, c + 1 < nk, c + 2 < nk ? BK : tail, wm, wn);
-            const uint32_t t = now;
-            now = next;
-            next = t;
+        // S - 1 chunks are on their way before the first is used. At chunk c's barrier
+        // every wave has loaded chunks c and c + 1 and read all of chunk c - 1, whose
+        // stage chunk c + S - 1 takes. (Past the last chunk zeros are loaded, so that the
+        // waits stay the same.)
+        constexpr bool AHEAD = S > 2;
+        constexpr int PER = TA::PARTS * TA::LOADS + TB::PARTS * TB::LOADS;
+        int64_t left = ke - kb;   // k from the chunk to be loaded next to the end
+        Frags<NP, NJ, MI> f[2];
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) {
+            uint16_t *d = lds + s * STAGE;
+            if (left >= BK) load_some<false, 0, PER>(a, b, d, d + TA::ELEMS, BK);
+            else load_some<true, 0, PER>(a, b, d, d + TA::ELEMS, (int)left);
+            a.base += a.step;
+            b.base += b.step;
+            left -= BK;
         }
+        if constexpr (AHEAD) {
+            loaded_all_but<PER *(S - 2)>();
+            f[0].template fetch<TA, TB>(lds, lds + TA::ELEMS, wm, wn, 0);
+        }
+        int now = 0;
+        auto chunk = [&](auto tail) __attribute__((always_inline)) {
+            loaded_all_but<AHEAD ? PER *(S - 3) : 0>();
+            if constexpr (!AHEAD) f[0].template fetch<TA, TB>(lds + now, lds + now + TA::ELEMS, wm, wn, 0);
+            const int last = now == 0 ? (S - 1) * STAGE : now - STAGE;
+            const int next = now == (S - 1) * STAGE ? 0 : now + STAGE;
+            chunk_step<decltype(tail)::value, AHEAD, T>(a, b, sum, f, lds + last, lds + last + TA::ELEMS, lds + now,
+                                                 lds + now + TA::ELEMS, lds + next, lds + next + TA::ELEMS,
+                                                 (int)left, wm, wn);
+            now = next;
+            a.base += a.step;
+            b.base += b.step;
+            left -= BK;
+        };
+        int c = 0;
+        for (; left >= BK; ++c) chunk(std::false_type());
+        for (; c < nk; ++c) chunk(std::true_type());
     }
 
     // The results, 32 rows of a wave at a time, through LDS: a lane's registers hold four
@@ -297,7 +375,7 @@ __global__ __launch_bounds__(256) void k_gemm_join(const GemmArgs g) {
     }
 }
 
-template <class T, int OP, int TM, int TN, int BK, int WM, int WN>
+template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN>
 static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream) {
     constexpr int64_t CUS = 256;
     g.tiles_m = (int)ceil_div(g.M, TM);
@@ -309,7 +387,7 @@ static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream
     if (splits < 1) splits = 1;
     g.kc = ceil_div(chunks, splits) * BK;
     g.splits = g.K > 0 ? (int)ceil_div(g.K, g.kc) : 1;
-    hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, WM, WN>), dim3((unsigned)(tiles * g.splits)),
+    hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, S, WM, WN>), dim3((unsigned)(tiles * g.splits)),
                        dim3(64 * WM * WN), 0, stream, g);
     if (hipError_t e = hipGetLastError()) return e;
     if (g.splits > 1) {
@@ -323,13 +401,13 @@ template <class T, int OP>
 static hipError_t gemm_op(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
     const int64_t big = ceil_div(g.M, 256) * ceil_div(g.N, 256), mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
     if constexpr (sizeof(T) == 2) {
-        if (big >= 200) return gemm_tiles<T, OP, 256, 256, 64, 2, 4>(g, part_floats, stream);
-        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 64, 2, 2>(g, part_floats, stream);
-        return gemm_tiles<T, OP, 64, 64, 64, 2, 2>(g, part_floats, stream);
+        if (big >= 200) return gemm_tiles<T, OP, 256, 256, OP == GEMM_TN ? 32 : 64, OP == GEMM_TN ? 5 : 2, 2, 4>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 4, 2, 2>(g, part_floats, stream);
+        return gemm_tiles<T, OP, 64, 64, 64, 4, 2, 2>(g, part_floats, stream);
     } else {
-        if (mid >= 400) return gemm_tiles<T, OP, 256, 128, 32, 4, 2>(g, part_floats, stream);
-        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 2, 2>(g, part_floats, stream);
-        return gemm_tiles<T, OP, 64, 64, 32, 2, 2>(g, part_floats, stream);
+        if (mid >= 400) return gemm_tiles<T, OP, 256, 128, 32, 2, 4, 2>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 3, 2, 4>(g, part_floats, stream);
+        return gemm_tiles<T, OP, 64, 64, 32, 4, 2, 2>(g, part_floats, stream);
     }
 }
 
