@@ -29,17 +29,24 @@ __device__ __forceinline__ float up(float v) { return v; }
 __device__ __forceinline__ float up(bf16 v) { return (float)v; }
 __device__ __forceinline__ float up(f16 v) { return (float)v; }
 
-// columns [c, c + 8) of the row at p into v; columns from n on read nothing and give 0
+// columns [c, c + 8) of the row at p; columns from n on read nothing and give 0
 template <class T>
-__device__ __forceinline__ void load8(const T *p, int64_t c, int64_t n, float (&v)[8]) {
+__device__ __forceinline__ Oct<T> fetch8(const T *p, int64_t c, int64_t n) {
+    Oct<T> o;
     if (c + 8 <= n) {
-        const Oct<T> o = *reinterpret_cast<const Oct<T> *>(p + c);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = up(o.e[j]);
+        o = *reinterpret_cast<const Oct<T> *>(p + c);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < n ? up(p[c + j]) : 0.0f;
+        for (int j = 0; j < 8; ++j) o.e[j] = c + j < n ? p[c + j] : (T)0.0f;
     }
+    return o;
+}
+
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int64_t c, int64_t n, float (&v)[8]) {
+    const Oct<T> o = fetch8(p, c, n);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = up(o.e[j]);
 }
 
 // v, rounded once, to columns [c, c + 8) of the row at p, as far as they are below n

@@ -319,37 +319,52 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
     }
 
     // The results, 32 rows of a wave at a time, through LDS: a lane's registers hold four
-    // columns here and there of one row, memory is read and written along the rows.
+    // columns here and there of one row, memory is read and written along the rows. A
+    // lane's columns are the same in all rows; the residual's rows are read ahead.
     __syncthreads();
     float *C = reinterpret_cast<float *>(lds) + wave * 32 * CS;
-    DropState st;
-    if (g.e.drop.rng) st.init(g.e.drop, g.N);
-#pragma unroll
+    constexpr int GROUPS = WTN / 8, ROWS = 64 / GROUPS, ITERS = 32 / ROWS;
+    const int lr = lane / GROUPS;
+    const int64_t m1 = m0 + wm + lr, n = n0 + wn + 8 * (lane % GROUPS);
+    const bool whole = g.splits == 1;
+    Finish<T> fin;
+    if (whole) fin.init(g.e, n, g.N);
+#pragma unroll 1
     for (int i = 0; i < MI; ++i) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int ii = 0; ii < MI; ++ii)
+            if (ii == i) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                f4 v;
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    v[r] = acc[j][i][4 * q + r];
-                    if constexpr (NP == 3) v[r] += lo[j][i][4 * q + r];
-                }
-                *reinterpret_cast<f4 *>(C + (lane & 31) * CS + 32 * j + 8 * q + 4 * (lane >> 5)) = v;
+                    for (int q = 0; q < 4; ++q) {
+                        f4 v;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            v[r] = acc[j][ii][4 * q + r];
+                            if constexpr (NP == 3) v[r] += lo[j][ii][4 * q + r];
+                        }
+                        *reinterpret_cast<f4 *>(C + (lane & 31) * CS + 32 * j + 8 * q + 4 * (lane >> 5)) = v;
+                    }
             }
-        wave_sync();
-        constexpr int GROUPS = WTN / 8, ROWS = 64 / GROUPS;
-#pragma unroll 1
-        for (int r = lane / GROUPS; r < 32; r += ROWS) {
-            const int64_t m = m0 + wm + 32 * i + r, n = n0 + wn + 8 * (lane % GROUPS);
-            if (m >= g.M || n >= g.N) continue;
-            float v[8];
-            const f4 *c = reinterpret_cast<const f4 *>(C + r * CS + 8 * (lane % GROUPS));
+        const int64_t m = m1 + 32 * i;
+        Oct<T> res[ITERS];
+        if (whole && g.e.R) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = c[k / 4][k % 4];
-            if (g.splits > 1) store8(g.part + ((int64_t)split * g.M + m) * g.N, n, g.N, v);
-            else finish8<T>(g.e, st, m, n, g.N, v);
+            for (int k = 0; k < ITERS; ++k)
+                if (m + k * ROWS < g.M && n < g.N) res[k] = fetch8((const T *)g.e.R + (m + k * ROWS) * g.e.ldr, n, g.N);
+        }
+        wave_sync();
+#pragma unroll
+        for (int k = 0; k < ITERS; ++k) {
+            const int64_t r = m + k * ROWS;
+            if (r >= g.M || n >= g.N) continue;
+            float v[8];
+            const f4 *c = reinterpret_cast<const f4 *>(C + (lr + k * ROWS) * CS + 8 * (lane % GROUPS));
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] = c[x / 4][x % 4];
+            if (!whole) store8(g.part + ((int64_t)split * g.M + r) * g.N, n, g.N, v);
+            else fin.finish(g.e, r, n, g.N, v, res[k]);
         }
         wave_sync();
     }
@@ -358,20 +373,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
 // The splits' sums, in order, through the epilogue.
 template <class T>
 __global__ __launch_bounds__(256) void k_gemm_join(const GemmArgs g) {
-    DropState st;
-    if (g.e.drop.rng) st.init(g.e.drop, g.N);
     const int64_t blocks = (g.N + 7) / 8, total = g.M * blocks, step = (int64_t)gridDim.x * 256;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
         const int64_t m = i / blocks, n = (i - m * blocks) * 8;
+        Finish<T> fin;
+        fin.init(g.e, n, g.N);
+        Oct<T> res;
+        if (g.e.R) res = fetch8((const T *)g.e.R + m * g.e.ldr, n, g.N);
         float v[8];
         load8(g.part + m * g.N, n, g.N, v);
+#pragma unroll 4
         for (int s = 1; s < g.splits; ++s) {
             float w[8];
             load8(g.part + (s * g.M + m) * g.N, n, g.N, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += w[j];
         }
-        finish8<T>(g.e, st, m, n, g.N, v);
+        fin.finish(g.e, m, n, g.N, v, res);
     }
 }
 
@@ -401,12 +419,15 @@ template <class T, int OP>
 static hipError_t gemm_op(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
     const int64_t big = ceil_div(g.M, 256) * ceil_div(g.N, 256), mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
     if constexpr (sizeof(T) == 2) {
-        if (big >= 200) return gemm_tiles<T, OP, 256, 256, OP == GEMM_TN ? 32 : 64, OP == GEMM_TN ? 5 : 2, 2, 4>(g, part_floats, stream);
-        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 4, 2, 2>(g, part_floats, stream);
+        constexpr bool TN = OP == GEMM_TN;
+        if (big >= 200) return gemm_tiles<T, OP, 256, 256, TN ? 32 : 64, TN ? 5 : 2, 2, 4>(g, part_floats, stream);
+        if constexpr (!TN)
+            if (mid >= 400) return gemm_tiles<T, OP, 128, 128, 64, 2, 2, 2>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, TN ? 32 : 64, 4, 2, TN ? 2 : 4>(g, part_floats, stream);
         return gemm_tiles<T, OP, 64, 64, 64, 4, 2, 2>(g, part_floats, stream);
     } else {
         if (mid >= 400) return gemm_tiles<T, OP, 256, 128, 32, 2, 4, 2>(g, part_floats, stream);
-        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 3, 2, 4>(g, part_floats, stream);
+        if (mid >= 32) return gemm_tiles<T, OP, 128, 128, 32, 2, 2, 4>(g, part_floats, stream);
         return gemm_tiles<T, OP, 64, 64, 32, 4, 2, 2>(g, part_floats, stream);
     }
 }

@@ -20,28 +20,35 @@ struct Epilogue {
     Drop drop;
 };
 
-// The sums of columns [c, c + 8) of row r, c a multiple of 8; columns from n on are not
-// touched.
+// The epilogue of columns [c, c + 8), c a multiple of 8, for a lane that takes them of
+// several rows. Columns from n on are not touched.
 template <class T>
-__device__ __forceinline__ void finish8(const Epilogue &e, const DropState &st, int64_t r, int64_t c,
-                                        int64_t n, float (&v)[8]) {
-    if (e.bias) {
-        float b[8];
-        load8((const T *)e.bias, c, n, b);
+struct Finish {
+    float bias[8];
+    DropState drop;
+    __device__ __forceinline__ void init(const Epilogue &e, int64_t c, int64_t n) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += b[j];
+        for (int j = 0; j < 8; ++j) bias[j] = 0.0f;
+        if (e.bias && c < n) load8((const T *)e.bias, c, n, bias);
+        if (e.drop.rng) drop.init(e.drop, n);
     }
-    if (e.Z) store8((T *)e.Z + r * e.ldz, c, n, v);
-    activate8(e.act, v);
-    if (e.drop.rng) drop8(st.bits(r, c), e.drop.threshold, e.drop.scale, v);
-    if (e.R) {
-        float q[8];
-        load8((const T *)e.R + r * e.ldr, c, n, q);
+    // v: the sums of row r; res: the row's residual
+    __device__ __forceinline__ void finish(const Epilogue &e, int64_t r, int64_t c, int64_t n, float (&v)[8],
+                                           const Oct<T> &res) const {
+        if (e.bias) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += q[j];
+            for (int j = 0; j < 8; ++j) v[j] += bias[j];
+        }
+        if (e.Z) store8((T *)e.Z + r * e.ldz, c, n, v);
+        activate8(e.act, v);
+        if (e.drop.rng) drop8(drop.bits(r, c), e.drop.threshold, e.drop.scale, v);
+        if (e.R) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += up(res.e[j]);
+        }
+        store8((T *)e.Y + r * e.ldy, c, n, v);
     }
-    store8((T *)e.Y + r * e.ldy, c, n, v);
-}
+};
 
 // An operand of a product on the matrix cores, as 16-bit values: rows of `ld` elements,
 // 16-byte aligned, ld and the length of a row multiples of 8 (what pads a row is zero).
