@@ -377,8 +377,10 @@ size_t mlp_linear_workspace_bytes(int32_t dtype, int64_t d_in, int64_t d_out, in
  *   workspace   device buffer of at least mlp_linear_workspace_bytes bytes, 256-byte
  *               aligned, kept alive for the life of the context
  *   stream      hipStream_t of that device to enqueue on (NULL = the null stream)
- * Nothing is enqueued. *out is set only on success. Calls on one context must not
- * overlap, nor replays of graphs that hold calls on it (they share the workspace). */
+ * Enqueues a clear of the workspace's control words on `stream`; later calls must be
+ * ordered after it (same stream, or a synchronisation), and after one another: calls on
+ * one context must not overlap, nor replays of graphs that hold calls on it (they share
+ * the workspace). *out is set only on success. */
 typedef struct mlp_linear_ctx *mlp_linear_t;
 mlp_status mlp_linear_init(mlp_linear_t *out, int32_t dtype, int64_t d_in, int64_t d_out,
                            int32_t activation, int64_t max_rows, const void *W, const void *bias,

@@ -13,6 +13,7 @@ namespace mlp {
 
 constexpr int64_t LINEAR_MAX_WIDTH = 1 << 20;
 constexpr int COL_CHUNKS = 256;                   // most row chunks of the column sums
+constexpr int64_t ARRIVED_WORDS = 16384;
 constexpr int64_t PART_FLOATS_MAX = 256 * 65536;  // 256 workgroups' tiles of partial sums
 
 struct LinearCtx {
@@ -22,9 +23,12 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     uint16_t *g = nullptr, *x = nullptr, *w = nullptr;
+    uint16_t *g_few = nullptr;  // fp32: the parts of g where g itself is fp32 (up to 64 rows)
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
+    uint32_t *arrived = nullptr;   // the few-row products' arrival counts, zero between calls
+    int64_t arrived_words = 0;
     hipStream_t stream = nullptr;
     int device = 0;
 };
@@ -69,7 +73,9 @@ __global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t ro
 struct GradArgs {
     const void *Z, *dY;
     uint16_t *G;              // nullable, an operand of rows of pad8(N)
+    bool parts;               // of an fp32 layer: G in its three parts, else as fp32
     float *col;               // nullable [chunks x N]
+    void *db;                 // nullable [N], of a single chunk
     int64_t ldz, lddy, plane, M, N, chunk;   // chunk: rows of a workgroup
     int groups;               // a power of two up to 32
     int act;
@@ -100,12 +106,15 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = c + j < a.N ? v[j] : 0.0f;
             }
-            if (a.G) put8<T>(a.G + r * ldg + c, a.plane, v);
+            if (a.G) {
+                if (sizeof(T) == 2 || a.parts) put8<T>(a.G + r * ldg + c, a.plane, v);
+                else store8((T *)a.G + r * ldg, c, ldg, v);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
         }
     }
-    if (!a.col) return;
+    if (!a.col && !a.db) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) part[t][j] = sum[j];
     __syncthreads();
@@ -118,8 +127,11 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
     }
     if (t < a.groups) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c + j < a.N) a.col[(int64_t)blockIdx.x * a.N + c + j] = part[t][j];
+        for (int j = 0; j < 8; ++j) {
+            if (c + j >= a.N) continue;
+            if (a.db) ((T *)a.db)[c + j] = (T)part[t][j];
+            else a.col[(int64_t)blockIdx.x * a.N + c + j] = part[t][j];
+        }
     }
 }
 
@@ -164,7 +176,8 @@ static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t 
            d_out <= LINEAR_MAX_WIDTH && max_rows >= 1 && max_rows <= MLP_MAX_BATCH;
 }
 
-// Workspace: the operands g, X and W, the partial column sums, the partial products.
+// Workspace: the operands g, X and W, the partial column sums, the partial products, the
+// arrival counts.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -175,6 +188,7 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const size_t element = c->dtype == MLP_F32 ? 6 : 2;
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
     c->g = (uint16_t *)take(element * M * pad8(N));
+    c->g_few = (uint16_t *)take(c->dtype == MLP_F32 ? element * 64 * pad8(N) : 0);
     c->x = (uint16_t *)take(element * M * pad8(K));
     c->w = (uint16_t *)take(element * K * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
@@ -182,6 +196,8 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     if (most < K * N) most = K * N;
     c->part_floats = most < PART_FLOATS_MAX / 256 ? 256 * most : PART_FLOATS_MAX;
     c->part = (float *)take(sizeof(float) * (size_t)c->part_floats);
+    c->arrived_words = ARRIVED_WORDS;
+    c->arrived = (uint32_t *)take(sizeof(uint32_t) * (size_t)c->arrived_words);
     return at;
 }
 
@@ -203,8 +219,17 @@ static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t
     return hipGetLastError();
 }
 
+// Whether the products of M rows go to linear_skinny.hip: those of a few rows, and in
+// fp32, where the tiles' operands would be packed first, small ones.
+static bool few_rows(const LinearCtx &c, int64_t M) {
+    return M <= 32 || (c.dtype == MLP_F32 && (M <= 64 || M * c.d_in * c.d_out <= (1 << 27)));
+}
+
 template <class T>
 static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx, int64_t rows, const Epilogue &e) {
+    if (few_rows(c, rows))
+        return launch_skinny(GEMM_NN, c.dtype, X, ldx, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
+                             c.part_floats, c.arrived, c.arrived_words, c.stream);
     Operand x, w;
     if (hipError_t s = operand<T>(c, X, ldx, rows, c.d_in, c.x, &x)) return s;
     if (hipError_t s = operand<T>(c, c.W, c.d_out, c.d_in, c.d_out, c.w, &w)) return s;
@@ -222,11 +247,12 @@ struct BackwardArgs {
 template <class T>
 static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     const int64_t M = b.rows, N = c.d_out, K = c.d_in;
-    const bool products = M > 0 && (b.dX || b.dW);
-    // without activation and dropout g is dY, and dY itself the operand
-    const bool same = c.act == MLP_ACT_NONE && !b.drop.rng;
+    const bool products = M > 0 && (b.dX || b.dW), few = few_rows(c, M);
+    // without activation and dropout g is dY, and dY itself the operand (of few rows, where
+    // 32-bit offsets reach over the depth of a step)
+    const bool same = c.act == MLP_ACT_NONE && !b.drop.rng && (!few || b.lddy < (1 << 24));
     Operand g{c.g, pad8(N), M * pad8(N)};
-    if (products && same)
+    if (products && same && !few)
         if (hipError_t e = operand<T>(c, b.dY, b.lddy, M, N, c.g, &g)) return e;
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
@@ -234,14 +260,16 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.groups = 1;
         while (a.groups < 32 && a.groups * 8 < N) a.groups *= 2;
         const int64_t step = 256 / a.groups;
-        // about four workgroups a compute unit
+        // about four workgroups a compute unit; few rows in one chunk, which gives db
         const int64_t want = ceil_div(1024, ceil_div(N, 8 * a.groups));
-        a.chunk = ceil_div(ceil_div(M, want < COL_CHUNKS ? want : COL_CHUNKS), step) * step;
+        a.chunk = M <= 64 ? M : ceil_div(ceil_div(M, want < COL_CHUNKS ? want : COL_CHUNKS), step) * step;
         chunks = ceil_div(M, a.chunk);
         a.Z = b.Z;
         a.dY = b.dY;
         a.G = products && !same ? c.g : nullptr;
-        a.col = b.db ? c.col : nullptr;
+        a.parts = !few;
+        a.col = b.db && chunks > 1 ? c.col : nullptr;
+        a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
         a.lddy = b.lddy;
         a.plane = g.plane;
@@ -253,13 +281,28 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
                            dim3(256), 0, c.stream, a);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    if (b.db) {
+    if (b.db && chunks != 1) {
         hipLaunchKernelGGL(k_column_sums<T>, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, c.stream, c.col,
                            chunks, N, (T *)b.db);
         if (hipError_t e = hipGetLastError()) return e;
     }
     Epilogue e{};
-    if (b.dX && M > 0) {
+    if (few) {
+        const void *G = same ? b.dY : c.g;
+        const int64_t ldg = same ? b.lddy : pad8(N);
+        e.Y = b.dX;
+        e.ldy = b.lddx;
+        if (b.dX && M > 0)
+            if (hipError_t s = launch_skinny(GEMM_NT, c.dtype, G, ldg, c.W, N, M, K, N, e, c.part,
+                                             c.part_floats, c.arrived, c.arrived_words, c.stream))
+                return s;
+        // (fp32 dW of 64 x 4,096 x 4,096: 59 us here, 37 on tiles, parts and all; of 128 x
+        // 1,024 x 1,024 10 us and 16)
+        if (!b.dW || M <= 32 || M * K * N <= (1 << 27))
+            return b.dW ? launch_outer(c.dtype, b.X, b.ldx, G, ldg, M, K, N, b.dW, c.stream) : hipSuccess;
+        if (hipError_t s = operand<T>(c, G, ldg, M, N, c.g_few, &g)) return s;
+    }
+    if (b.dX && !few) {
         Operand w;
         if (hipError_t s = operand<T>(c, c.W, N, K, N, c.w, &w)) return s;
         e.Y = b.dX;
@@ -276,6 +319,10 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
             return s;
     }
     return hipSuccess;
+}
+
+__global__ __launch_bounds__(256) void k_clear(uint32_t *p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
 }  // namespace mlp
@@ -313,7 +360,13 @@ extern "C" mlp_status mlp_linear_init(mlp_linear_t *out, int32_t dtype, int64_t 
     c->bias = bias;
     c->stream = (hipStream_t)stream;
     linear_carve(c, (char *)workspace);
-    if (hipGetDevice(&c->device) != hipSuccess) {
+    hipError_t e = hipGetDevice(&c->device);
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(k_clear, dim3((unsigned)ceil_div(c->arrived_words, 256)), dim3(256), 0, c->stream,
+                           c->arrived, c->arrived_words);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) {
         delete c;
         return MLP_ERR_HIP;
     }

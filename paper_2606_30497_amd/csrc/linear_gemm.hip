@@ -203,7 +203,7 @@ __device__ __forceinline__ void chunk_step(const TA &a, const TB &b, Sums<NP, NJ
                                            uint16_t *__restrict__ Bn, const uint16_t *__restrict__ Ac,
                                            const uint16_t *__restrict__ Bc, const uint16_t *__restrict__ Af,
                                            const uint16_t *__restrict__ Bf, int left, int wm, int wn) {
-    constexpr int KK = TA::K / 16, SLOTS = AHEAD ? KK * NJ : 3 * KK * NJ / 8;
+    constexpr int KK = TA::K / 16, SLOTS = AHEAD ? KK * NJ : (3 * KK * NJ + 7) / 8;
     constexpr int ALL = TA::PARTS * TA::LOADS + TB::PARTS * TB::LOADS;
     constexpr int MFMAS = MI * (NP == 3 ? 6 : 1);
     constexpr int EACH = 2;   // LDS reads after a product

@@ -1,0 +1,441 @@
+// linear_skinny.hip -- the dense layer's matrix products that are bound by W or by latency:
+// of few rows (single tokens, small batches), and small ones in fp32.
+//
+// k_skinny, y = x W and dX = g W^T: W goes from memory straight to the registers of the
+// matrix cores, 128 outputs and 32 (fp32: 16) of the depth a wave and step, two steps
+// ahead, at any alignment; a workgroup takes 16 or 32 rows, and nothing is shared, so LDS
+// has no part in it. The waves of a workgroup and `splits` workgroups share the depth; a
+// workgroup adds its waves' sums in LDS, and the last of the splits to arrive adds theirs,
+// in order, and finishes the rows. The products are v_mfma_f32_16x16x32 of 16-bit values,
+// v_mfma_f32_16x16x4f32 of fp32 ones (plain fp32 products), W as the first operand: its row
+// r of product t is output 8 r + t, so that a lane's results of the eight products are
+// eight columns in a row. Where W's rows lie along the outputs, a lane loads eight
+// outputs of eight (fp32: four) k and the pairs of k are put together by v_perm.
+//
+// k_outer, dW = X^T g of few rows: the same products with X read across its rows; a wave
+// takes 16 x 128 values of dW, bound by writing them.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "linear_internal.h"
+
+namespace mlp {
+
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+
+constexpr int SKINNY_N = 128;   // outputs of a workgroup
+
+struct SkinnyArgs {
+    const void *X, *W;
+    int64_t ldx, ldw, M, N, K;
+    int splits;
+    int64_t kw;            // depth of a wave (a multiple of the step)
+    float *part;           // [splits][M][N rounded up to SKINNY_N]
+    uint32_t *arrived;     // [row tiles][output tiles], zero between calls
+    Epilogue e;
+};
+
+template <class T>
+__device__ __forceinline__ f4 mma16(u4v a, u4v b, f4 c) {
+    if constexpr (std::is_same<T, bf16>::value) return mfma_bf16(a, b, c);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8v, a), __builtin_bit_cast(h8v, b), c, 0, 0, 0);
+}
+
+// 16 bytes at any element's address
+template <class T>
+struct __attribute__((packed, aligned(sizeof(T)))) Piece {
+    uint32_t w[4];
+    __device__ __forceinline__ u4v get() const { return u4v{w[0], w[1], w[2], w[3]}; }
+};
+
+// One step of a wave's depth: W for 128 outputs, X for 16 MT rows.
+// 16-bit: w[i] = outputs 8 r .. + 7 of k 8 g + i (OUT: W's rows lie along the outputs), or k
+// 8 g .. + 7 of output 8 r + i. fp32: w[2 s + h] = outputs 8 r + 4 h .. + 3 of k 4 g + s, or
+// w[i] = k 4 g .. + 3 of output 8 r + i. (Lane l: r = l % 16, g = l / 16.)
+template <class T, bool OUT, int MT>
+struct Step {
+    static constexpr int PER = 16 / sizeof(T), K = 4 * PER;   // elements of a piece, depth
+    u4v w[8], x[MT];
+
+    static __device__ __forceinline__ u4v piece(const char *p, uint32_t off) {
+        return reinterpret_cast<const Piece<T> *>(p + off)->get();
+    }
+    // PER elements from p + off on, of which n >= 1 are inside; those past them are read
+    // from the last one and, if `zero`, set to 0
+    static __device__ __forceinline__ u4v edge(const char *p, uint32_t off, int n, bool zero) {
+        union {
+            T e[PER];
+            u4v v;
+        } o;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const T e = *reinterpret_cast<const T *>(p + (off + (uint32_t)(j < n ? j : n - 1) * (uint32_t)sizeof(T)));
+            o.e[j] = zero && j >= n ? (T)0.0f : e;
+        }
+        return o.v;
+    }
+    // The step at depth k0 (uniform) of the outputs from n0 on. EDGE: the tile reaches past
+    // the outputs; TAIL: the step reaches past the depth. What lies outside is read from
+    // the last row or column inside; past the depth it counts as 0.
+    template <bool EDGE, bool TAIL>
+    __device__ __forceinline__ void load(const void *W, int64_t ld, int64_t N, int64_t depth_all, int64_t n0, int64_t k0) {
+        const int l = threadIdx.x & 63, r = l & 15, g = l >> 4;
+        const uint32_t ES = sizeof(T), ldw = (uint32_t)ld * ES;
+        const int nl = (int)(N - n0 < SKINNY_N ? N - n0 : SKINNY_N);   // outputs of the tile
+        const int kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);                 // depth of the step
+        const char *base = (const char *)W + (OUT ? k0 * ld + n0 : n0 * ld + k0) * ES;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (OUT) {
+                const int kd = sizeof(T) == 2 ? i : i / 2, k = PER * g + kd;
+                const int n = 8 * r + (sizeof(T) == 2 ? 0 : 4 * (i & 1));
+                const char *row = base;
+                uint32_t off = (uint32_t)(PER * g) * ldw;
+                if constexpr (TAIL) off = (uint32_t)(k < kl ? k : kl - 1) * ldw;
+                else row += kd * (int64_t)ldw;
+                if constexpr (EDGE) {
+                    const int at = n < nl ? n : nl - 1;
+                    w[i] = edge(row, off + at * ES, nl - at, false);
+                } else {
+                    w[i] = piece(row, off + n * ES);
+                }
+                if (TAIL && k >= kl) w[i] = u4v{0, 0, 0, 0};
+            } else {
+                const char *row = base;
+                uint32_t off = (uint32_t)(8 * r) * ldw;
+                if constexpr (EDGE) off = (uint32_t)(8 * r + i < nl ? 8 * r + i : nl - 1) * ldw;
+                else row += i * (int64_t)ldw;
+                w[i] = TAIL ? depth(row + off, PER * g, kl) : piece(row, off + PER * g * ES);
+            }
+        }
+    }
+    // X's rows at xp (one for each 16 rows), k contiguous
+    template <bool TAIL>
+    __device__ __forceinline__ void load_x(const char *const (&xp)[MT], int64_t depth_all, int64_t k0) {
+        const int g = (threadIdx.x & 63) >> 4, kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            x[t] = TAIL ? depth(xp[t] + k0 * (int64_t)sizeof(T), PER * g, kl)
+                        : piece(xp[t] + k0 * (int64_t)sizeof(T), PER * g * (uint32_t)sizeof(T));
+    }
+    // X's columns at xp, k down them, `pitch` bytes apart
+    template <bool TAIL>
+    __device__ __forceinline__ void load_across(const char *const (&xp)[MT], int64_t pitch, int64_t depth_all,
+                                                int64_t k0) {
+        const int g = (threadIdx.x & 63) >> 4, kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            union {
+                T e[PER];
+                u4v v;
+            } o;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int k = PER * g + j;
+                const T e = *reinterpret_cast<const T *>(xp[t] + (k0 + (TAIL && k >= kl ? kl - 1 : k)) * pitch);
+                o.e[j] = TAIL && k >= kl ? (T)0.0f : e;
+            }
+            x[t] = o.v;
+        }
+    }
+    // elements [k, k + PER) of a row of kl >= 1, those past its end 0
+    static __device__ __forceinline__ u4v depth(const char *row, int k, int kl) {
+        const int at = k < kl ? k : kl - 1;
+        const u4v v = edge(row, (uint32_t)(at * (int)sizeof(T)), kl - at, true);
+        return k < kl ? v : u4v{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void multiply(f4 (&acc)[MT][8]) const {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            if constexpr (sizeof(T) == 2) {
+                u4v f = w[t];
+                if constexpr (OUT) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        f[q] = __builtin_amdgcn_perm(w[2 * q + 1][t >> 1], w[2 * q][t >> 1], t & 1 ? 0x07060302 : 0x05040100);
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[m][t] = mma16<T>(f, x[m], acc[m][t]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const float f = __uint_as_float(OUT ? w[2 * s + (t >> 2)][t & 3] : w[t][s]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f, __uint_as_float(x[m][s]), acc[m][t], 0, 0, 0);
+                }
+            }
+        }
+    }
+};
+
+template <class T, bool OUT, int MT, bool EDGE>
+__device__ __forceinline__ void skinny_sums(const SkinnyArgs &a, int64_t m0, int64_t n0, int64_t kb, f4 (&acc)[MT][8]) {
+    typedef Step<T, OUT, MT> S;
+    const int64_t ke = kb + a.kw < a.K ? kb + a.kw : a.K;
+    const int full = ke > kb ? (int)((ke - kb) / S::K) : 0;
+    const char *xp[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = m0 + 16 * t + (threadIdx.x & 15);
+        xp[t] = (const char *)a.X + (m < a.M ? m : a.M - 1) * a.ldx * (int64_t)sizeof(T);
+    }
+    auto load = [&](S &s, int i) __attribute__((always_inline)) {
+        const int64_t k0 = kb + i * (int64_t)S::K;
+        s.template load<EDGE, false>(a.W, a.ldw, a.N, a.K, n0, k0);
+        s.template load_x<false>(xp, a.K, k0);
+    };
+    if constexpr (EDGE) {
+        S s;
+#pragma unroll 1
+        for (int i = 0; i < full; ++i) {
+            load(s, i);
+            s.multiply(acc);
+        }
+    } else {
+        S s[2];
+        if (full > 0) load(s[0], 0);
+        if (full > 1) load(s[1], 1);
+        int i = 0;
+        for (; i + 2 <= full; i += 2) {
+            s[0].multiply(acc);
+            if (i + 2 < full) load(s[0], i + 2);
+            s[1].multiply(acc);
+            if (i + 3 < full) load(s[1], i + 3);
+        }
+        if (i < full) s[0].multiply(acc);
+    }
+    if (kb + (int64_t)full * S::K < ke) {
+        S s;
+        s.template load<EDGE, true>(a.W, a.ldw, a.N, a.K, n0, kb + (int64_t)full * S::K);
+        s.template load_x<true>(xp, a.K, kb + (int64_t)full * S::K);
+        s.multiply(acc);
+    }
+}
+
+template <class T, bool OUT, int MT>
+__global__ __launch_bounds__(512, 2) void k_skinny(const SkinnyArgs a) {
+    constexpr int WAVES = 8, NT = 512, CS = SKINNY_N + 4;
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][16 * MT][CS];
+    __shared__ uint32_t before;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int64_t n0 = (int64_t)tile * SKINNY_N, m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int rows = (int)(a.M - m0 < 16 * MT ? a.M - m0 : 16 * MT);
+    const int64_t kb = ((int64_t)split * WAVES + wave) * a.kw;
+    f4 acc[MT][8];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[m][t] = f4{0.f, 0.f, 0.f, 0.f};
+    if (n0 + SKINNY_N <= a.N) skinny_sums<T, OUT, MT, false>(a, m0, n0, kb, acc);
+    else skinny_sums<T, OUT, MT, true>(a, m0, n0, kb, acc);
+
+    // register v of product t: row l % 16, column 8 (4 (l / 16) + v) + t
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+        if (16 * m + (lane & 15) < rows) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f4 w{acc[m][4 * h][v], acc[m][4 * h + 1][v], acc[m][4 * h + 2][v], acc[m][4 * h + 3][v]};
+                    *reinterpret_cast<f4 *>(&sums[wave][16 * m + (lane & 15)][8 * (4 * (lane >> 4) + v) + 4 * h]) = w;
+                }
+        }
+    __syncthreads();
+    const int64_t pitch = (a.N + SKINNY_N - 1) / SKINNY_N * SKINNY_N;
+    if (a.splits > 1) {
+        for (int i = threadIdx.x; i < rows * SKINNY_N; i += NT) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) s += sums[w][i / SKINNY_N][i % SKINNY_N];
+            __hip_atomic_store(a.part + ((int64_t)split * a.M + m0 + i / SKINNY_N) * pitch + n0 + i % SKINNY_N, s,
+                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        // The sums are stored and read device-coherently, past the XCDs' own L2s, so their
+        // completion before the arrival is counted is all the order they need (a release
+        // at device scope would write back the whole L2: 45 us a call of 1 x 4,096 x 4,096
+        // with it, 8 without).
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        uint32_t *arrived = a.arrived + (int64_t)blockIdx.y * (pitch / SKINNY_N) + tile;
+        if (threadIdx.x == 0)
+            before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (before != (uint32_t)a.splits - 1) return;
+        if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    for (int i = threadIdx.x; i < rows * (SKINNY_N / 8); i += NT) {
+        const int r = i / (SKINNY_N / 8), c = i % (SKINNY_N / 8) * 8;
+        const int64_t n = n0 + c, m = m0 + r;
+        if (n >= a.N) continue;
+        Finish<T> fin;
+        fin.init(a.e, n, a.N);
+        Oct<T> res;
+        if (a.e.R) res = fetch8((const T *)a.e.R + m * a.e.ldr, n, a.N);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (a.splits > 1) {
+#pragma unroll 4
+            for (int s = 0; s < a.splits; ++s) {
+                const uint64_t *p = reinterpret_cast<const uint64_t *>(a.part + ((int64_t)s * a.M + m) * pitch + n);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t w = __hip_atomic_load(p + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    v[2 * j] += __uint_as_float((uint32_t)w);
+                    v[2 * j + 1] += __uint_as_float((uint32_t)(w >> 32));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += sums[w][r][c + j];
+        }
+        fin.finish(a.e, m, n, a.N, v, res);
+    }
+}
+
+template <class T, bool OUT, int MT>
+static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
+    constexpr int64_t STEP = Step<T, OUT, MT>::K;
+    const int64_t tiles = ceil_div(a.N, SKINNY_N), row_tiles = ceil_div(a.M, 16 * MT), pitch = tiles * SKINNY_N;
+    // A workgroup for each compute unit, of at least two steps a wave. (With 512 of them
+    // half wait for the other half, whose eight waves' registers fill the unit: fp32 1 x
+    // 4,096 x 4,096 16 us with 256, 22 with 512, 20 with 128.)
+    int64_t splits = ceil_div(a.K, 2 * STEP * 8);
+    if (splits > 256 / (tiles * row_tiles)) splits = 256 / (tiles * row_tiles);
+    if (splits > part_floats / (a.M * pitch)) splits = part_floats / (a.M * pitch);
+    if (splits < 1 || tiles * row_tiles > arrived_words) splits = 1;
+    a.kw = ceil_div(ceil_div(a.K, splits * 8), STEP) * STEP;
+    a.splits = (int)ceil_div(a.K, a.kw * 8);
+    hipLaunchKernelGGL((k_skinny<T, OUT, MT>), dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles), dim3(512), 0,
+                       stream, a);
+    return hipGetLastError();
+}
+
+template <class T, bool OUT>
+static hipError_t skinny_rows(const SkinnyArgs &a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
+    if (a.M <= 16) return skinny<T, OUT, 1>(a, part_floats, arrived_words, stream);
+    return skinny<T, OUT, 2>(a, part_floats, arrived_words, stream);
+}
+
+hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t ldw,
+                         int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part, int64_t part_floats,
+                         uint32_t *arrived, int64_t arrived_words, hipStream_t stream) {
+    const SkinnyArgs a{X, W, ldx, ldw, M, N, K, 1, 0, part, arrived, e};
+    const bool out = op == GEMM_NN;
+#define SKINNY(T) \
+    (out ? skinny_rows<T, true>(a, part_floats, arrived_words, stream) \
+         : skinny_rows<T, false>(a, part_floats, arrived_words, stream))
+    return dtype == MLP_F32 ? SKINNY(float) : dtype == MLP_BF16 ? SKINNY(bf16) : SKINNY(f16);
+#undef SKINNY
+}
+
+// Element v of lane group g (of 16 lanes) and element g of group v change places.
+__device__ __forceinline__ void trade(f4 &x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) w[v] = __float_as_uint(x[v]);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const auto p = __builtin_amdgcn_permlane32_swap(w[v], w[v + 2], false, false);
+        w[v] = p[0];
+        w[v + 2] = p[1];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; v += 2) {
+        const auto p = __builtin_amdgcn_permlane16_swap(w[v], w[v + 1], false, false);
+        w[v] = p[0];
+        w[v + 1] = p[1];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = __uint_as_float(w[v]);
+}
+
+struct OuterArgs {
+    const void *X, *G;
+    void *dW;
+    int64_t ldx, ldg, M, K, N;
+    int tiles;   // tiles of 16 k a wave
+};
+
+template <class T, bool EDGE>
+__device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0) {
+    typedef Step<T, true, 1> S;
+    const int lane = threadIdx.x & 63;
+    const int64_t pitch = a.ldx * (int64_t)sizeof(T);
+    const bool once = a.M <= S::K;   // G's rows stay in the registers for all tiles
+    S s;
+    if (once && a.M > 0) s.template load<EDGE, true>(a.G, a.ldg, a.N, a.M, n0, 0);
+#pragma unroll 1
+    for (int i = 0; i < a.tiles && k0 < a.K; ++i, k0 += 16) {
+        const int64_t k = k0 + (lane & 15);
+        const char *xp[1] = {(const char *)a.X + (k < a.K ? k : a.K - 1) * (int64_t)sizeof(T)};
+        f4 acc[1][8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[0][t] = f4{0.f, 0.f, 0.f, 0.f};
+        if (once) {
+            if (a.M > 0) {
+                s.template load_across<true>(xp, pitch, a.M, 0);
+                s.multiply(acc);
+            }
+        } else {
+            int64_t m = 0;
+#pragma unroll 2
+            for (; m + S::K <= a.M; m += S::K) {
+                s.template load<EDGE, false>(a.G, a.ldg, a.N, a.M, n0, m);
+                s.template load_across<false>(xp, pitch, a.M, m);
+                s.multiply(acc);
+            }
+            if (m < a.M) {
+                s.template load<EDGE, true>(a.G, a.ldg, a.N, a.M, n0, m);
+                s.template load_across<true>(xp, pitch, a.M, m);
+                s.multiply(acc);
+            }
+        }
+        // Register v of lane group g is piece 4 g + v of the row: traded among the four
+        // groups, piece 4 v + g, so that a store's four lanes of a row write side by side.
+#pragma unroll
+        for (int t = 0; t < 8; ++t) trade(acc[0][t]);
+        if (k < a.K) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t n = n0 + 8 * (4 * v + (lane >> 4));
+                float w[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) w[t] = acc[0][t][v];
+                if (n < a.N) store8((T *)a.dW + k * a.N, n, a.N, w);
+            }
+        }
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_outer(const OuterArgs a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * SKINNY_N, k0 = ((int64_t)blockIdx.y * 4 + wave) * (16 * a.tiles);
+    if (n0 + SKINNY_N <= a.N) outer<T, false>(a, k0, n0);
+    else outer<T, true>(a, k0, n0);
+}
+
+hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t M,
+                        int64_t K, int64_t N, void *dW, hipStream_t stream) {
+    // about 1,024 workgroups of four waves
+    const int64_t across = ceil_div(N, SKINNY_N), tiles = ceil_div(ceil_div(K, 64) * across, 1024);
+    const OuterArgs a{X, G, dW, ldx, ldg, M, K, N, (int)(tiles < 16 ? tiles : 16)};
+    const dim3 grid((unsigned)across, (unsigned)ceil_div(K, 64 * a.tiles));
+    switch (dtype) {
+    case MLP_F32: hipLaunchKernelGGL(k_outer<float>, grid, dim3(256), 0, stream, a); break;
+    case MLP_BF16: hipLaunchKernelGGL(k_outer<bf16>, grid, dim3(256), 0, stream, a); break;
+    default: hipLaunchKernelGGL(k_outer<f16>, grid, dim3(256), 0, stream, a); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace mlp

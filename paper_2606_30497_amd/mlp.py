@@ -502,13 +502,13 @@ def _rng(rng, device):
 class LinearContext:
     """A dense layer's context bound to caller-owned W, bias and workspace."""
 
-    def __init__(self, handle, W, bias, workspace, activation, max_rows, stream):
+    def __init__(self, handle, W, bias, workspace, activation, max_rows, stream, bound):
         self.handle = handle
         self.W, self.bias, self.workspace = W, bias, workspace
         self.d_in, self.d_out = W.shape
         self.activation, self.max_rows = activation, max_rows
         self.stream = stream    # None: each call goes on the current stream
-        self.bound = stream     # the stream the library's context is on
+        self.bound = bound      # the stream the library's context is on
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -542,27 +542,36 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
         if workspace.device != W.device:
             raise ValueError("workspace is on %s, not on %s" % (workspace.device, W.device))
         _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
+        bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
         handle = _vp()
         _check("mlp_linear_init",
                lib.mlp_linear_init(ctypes.byref(handle), DTYPES[W.dtype], d_in, d_out,
                                    ACTIVATIONS[activation], max_rows, wp, bp, workspace.data_ptr(),
-                                   workspace.numel(), stream or 0))
-    return LinearContext(handle, W, bias, workspace, activation, max_rows, stream)
+                                   workspace.numel(), bound))
+    return LinearContext(handle, W, bias, workspace, activation, max_rows, stream, bound)
 
 
 def mlp_linear_set_stream(ctx: LinearContext, stream) -> None:
     """Later calls go on `stream` (None: on the current stream at each call)."""
-    _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, stream or 0))
-    ctx.stream, ctx.bound = stream, stream
+    if stream is not None:
+        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, stream))
+        ctx.bound = stream
+    ctx.stream = stream
 
 
 def _bind_stream(ctx):
-    """Put the context on the current stream where it has none of its own."""
-    if ctx.stream is None:
-        s = torch.cuda.current_stream(ctx.W.device).cuda_stream
-        if s != ctx.bound:
-            _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, s))
-            ctx.bound = s
+    """Put the context on the current stream where it has none of its own, behind the
+    calls it made on another one before (a stream that captures cannot wait for those:
+    there the capture's own start has to be behind them)."""
+    if ctx.stream is not None:
+        return
+    s = torch.cuda.current_stream(ctx.W.device)
+    if s.cuda_stream != ctx.bound:
+        if not torch.cuda.is_current_stream_capturing():
+            s.wait_stream(torch.cuda.ExternalStream(ctx.bound, device=ctx.W.device) if ctx.bound
+                          else torch.cuda.default_stream(ctx.W.device))
+        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, s.cuda_stream))
+        ctx.bound = s.cuda_stream
 
 
 def _new(ctx, *shape):

@@ -13,7 +13,7 @@ SHAPES = [(1, 1, 1, 0), (1, 32, 1, 0), (2, 5, 7, 3), (1, 256, 512, 0), (1, 1000,
           (33, 17, 2049, 5), (48, 520, 520, 0), (64, 256, 256, 0), (65, 255, 257, 0), (100, 1032, 72, 8),
           (128, 128, 128, 0), (129, 64, 1, 0), (200, 2056, 136, 0), (256, 512, 384, 0), (257, 96, 520, 16),
           (300, 513, 77, 1), (512, 1024, 256, 0), (1000, 40, 8, 0), (777, 136, 1000, 8), (1500, 8, 24, 0),
-          (2000, 264, 264, 0)]
+          (2000, 264, 264, 0), (40, 4104, 136, 0), (24, 130, 8200, 0), (1040, 1032, 2056, 0), (33, 4000, 4104, 0)]
 # activation, p, bias, residual, z kept
 OPTIONS = [("none", 0.0, False, False, False), ("relu", 0.0, True, True, True), ("gelu", 0.1, True, False, True),
            ("gelu_tanh", 0.5, False, True, False), ("silu", 0.3, True, True, True)]
@@ -81,6 +81,43 @@ def test_backward(mlp, dtype, rows, d_in, d_out, pad):  # noqa: F811
             for name, got, want in zip(("dx", "dw", "db"), out, (dx, dw, db)):
                 assert (got is None) == (name != need or want is None)
                 assert got is None or torch.equal(got, want), name
+
+
+# shapes of the larger tiles (200 of 256 x 256, 400 of 128 x 128), a depth that ends inside
+# a chunk, row tails; whole activations on the CPU would take minutes, so the 64-bit
+# reference is taken of a sample of rows and of columns
+@pytest.mark.parametrize("dtype,rows,d_in,d_out", [("bf16", 3900, 136, 3600), ("f16", 3600, 3336, 300),
+                                                   ("bf16", 3600, 4104, 3400), ("bf16", 2400, 264, 2700),
+                                                   ("f32", 2600, 328, 2600), ("f32", 1100, 2600, 2650)])
+def test_large_tiles(mlp, dtype, rows, d_in, d_out):  # noqa: F811
+    g = torch.Generator().manual_seed(rows)
+    W, b = _layer(g, d_in, d_out, dtype, True)
+    _, x = _rows(g, rows, d_in, dtype, 0)
+    _, z = _rows(g, rows, d_out, dtype, 0)
+    _, dy = _rows(g, rows, d_out, dtype, 0)
+    ctx = mlp.mlp_linear_init(W, b, "silu", max_rows=rows)
+    y, zz = mlp.mlp_linear_forward(ctx, x, save_z=True)
+    dx, dw, db = mlp.mlp_linear_backward(ctx, x, dy, z=z)
+    torch.cuda.synchronize()
+    at = torch.randperm(rows, generator=g)[:40].tolist() + [0, rows - 1]
+    ry, rz, by, bz = R.forward(x[at], W, b, None, "silu", 0.0, None, dtype)
+    R.check("y", y[at], ry, by)
+    R.check("z", zz[at], rz, bz)
+    ref, bound = R.backward(x[at], W, z[at], dy[at], "silu", 0.0, None, dtype)
+    R.check("dx", dx[at], ref["dx"], bound["dx"])
+    cols = torch.randperm(d_in, generator=g)[:24].tolist() + [0, d_in - 1]
+    ref, bound = R.backward(x[:, cols], W[cols], z, dy, "silu", 0.0, None, dtype)
+    R.check("dw", dw[cols], ref["dw"], bound["dw"])
+    R.check("db", db, ref["db"], bound["db"])
+    # every element, on the GPU in fp32: rows or tiles left out would be off by the whole
+    u = 16 * R.U[dtype] + 4 * R.E * (max(rows, d_in, d_out) + 32) ** 0.5
+    f = torch.nn.functional.silu(x.float() @ W.float() + b.float())
+    assert float((y.float() - f).norm() / f.norm()) <= u and float((y.float() - f).abs().max()) <= 8 * u * float(f.abs().max())
+    sg = torch.sigmoid(z.float())
+    gg = dy.float() * sg * (1 + z.float() * (1 - sg))
+    for got, want in ((dx, gg @ W.float().t()), (dw, x.float().t() @ gg)):
+        assert float((got.float() - want).norm() / want.norm()) <= u
+        assert float((got.float() - want).abs().max()) <= 8 * u * float(want.abs().max())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
