@@ -469,34 +469,44 @@ def _mat(t, name, dtype, device, rows, cols):
     """(pointer, row stride) of a [rows, cols] matrix whose rows are contiguous."""
     if t is None:
         return None, 0
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == (rows, cols):
+        sr, sc = t.stride()
+        if (sc == 1 or cols <= 1) and (sr >= cols or rows <= 1):
+            return t.data_ptr(), (sr if rows > 1 else cols)
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     if t.device != device:
         raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError("%s must be [%d, %d], is %s" % (name, rows, cols, list(t.shape)))
     if cols > 1 and t.stride(1) != 1:
         raise ValueError("the elements of a row of %s must be adjacent" % name)
-    if rows > 1 and t.stride(0) < cols:
-        raise ValueError("the rows of %s overlap" % name)
-    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+    raise ValueError("the rows of %s overlap" % name)
 
 
 def _vec(t, name, dtype, device, n):
     if t is None:
         return None
+    p = _dev(t, name, dtype=dtype)
     if t.device != device:
         raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
     if t.numel() != n:
         raise ValueError("%s has %d elements, needs %d" % (name, t.numel(), n))
-    return _dev(t, name, dtype=dtype)
+    return p
 
 
 def _rng(rng, device):
     """The generator's state: int64 [2] (seed, offset) in device memory."""
-    return _vec(rng, "rng", torch.int64, device, 2)
+    return None if rng is None else _vec(rng, "rng", torch.int64, device, 2)
+
+
+# The handle of the stream that is current on a device. (A call of a small layer takes
+# about 7 us of the host, half of it the launch; torch.cuda.current_stream, which makes an
+# object of the handle, would add 1.8.)
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class LinearContext:
@@ -506,6 +516,7 @@ class LinearContext:
         self.handle = handle
         self.W, self.bias, self.workspace = W, bias, workspace
         self.d_in, self.d_out = W.shape
+        self.dtype, self.device = W.dtype, W.device
         self.activation, self.max_rows = activation, max_rows
         self.stream = stream    # None: each call goes on the current stream
         self.bound = bound      # the stream the library's context is on
@@ -565,21 +576,22 @@ def _bind_stream(ctx):
     there the capture's own start has to be behind them)."""
     if ctx.stream is not None:
         return
-    s = torch.cuda.current_stream(ctx.W.device)
-    if s.cuda_stream != ctx.bound:
+    now = _current_stream(ctx.device.index)
+    if now != ctx.bound:
         if not torch.cuda.is_current_stream_capturing():
-            s.wait_stream(torch.cuda.ExternalStream(ctx.bound, device=ctx.W.device) if ctx.bound
-                          else torch.cuda.default_stream(ctx.W.device))
-        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, s.cuda_stream))
-        ctx.bound = s.cuda_stream
+            before = (torch.cuda.ExternalStream(ctx.bound, device=ctx.device) if ctx.bound
+                      else torch.cuda.default_stream(ctx.device))
+            torch.cuda.current_stream(ctx.device).wait_stream(before)
+        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
+        ctx.bound = now
 
 
 def _new(ctx, *shape):
     """An output of the context's type, its memory taken on the stream that writes it."""
     if ctx.stream is None:
-        return torch.empty(shape, dtype=ctx.W.dtype, device=ctx.W.device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.W.device)):
-        return torch.empty(shape, dtype=ctx.W.dtype, device=ctx.W.device)
+        return torch.empty(shape, dtype=ctx.dtype, device=ctx.device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.device)):
+        return torch.empty(shape, dtype=ctx.dtype, device=ctx.device)
 
 
 def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, out=None, z=None,
@@ -588,8 +600,7 @@ def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, ou
     bias, which the backward call takes: then (Y, z) is returned."""
     if X.dim() != 2:
         raise ValueError("X must be [rows, d_in]")
-    W, rows, n = ctx.W, X.shape[0], ctx.d_out
-    dev, dt = W.device, W.dtype
+    rows, n, dev, dt = X.shape[0], ctx.d_out, ctx.device, ctx.dtype
     xp, ldx = _mat(X, "X", dt, dev, rows, ctx.d_in)
     rp, ldr = _mat(residual, "residual", dt, dev, rows, n)
     gp = _rng(rng, dev)
@@ -600,8 +611,8 @@ def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, ou
     yp, ldy = _mat(out, "out", dt, dev, rows, n)
     zp, ldz = _mat(z, "z", dt, dev, rows, n)
     _bind_stream(ctx)
-    _check("mlp_linear_forward", load().mlp_linear_forward(ctx.handle, xp, ldx, rows, rp, ldr, float(p),
-                                                           gp, yp, ldy, zp, ldz))
+    _check("mlp_linear_forward", load().mlp_linear_forward(ctx.handle, xp, ldx, rows, rp, ldr, float(p), gp, yp,
+                                                           ldy, zp, ldz))
     return out if z is None else (out, z)
 
 
@@ -611,8 +622,7 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
     needed (db: for a layer without bias). X may be None where dW is not needed."""
     if dY.dim() != 2:
         raise ValueError("dY must be [rows, d_out]")
-    W, rows, n = ctx.W, dY.shape[0], ctx.d_out
-    dev, dt = W.device, W.dtype
+    rows, n, dev, dt = dY.shape[0], ctx.d_out, ctx.device, ctx.dtype
     xp, ldx = _mat(X, "X", dt, dev, rows, ctx.d_in)
     gyp, lddy = _mat(dY, "dY", dt, dev, rows, n)
     zp, ldz = _mat(z, "z", dt, dev, rows, n)
@@ -628,28 +638,33 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
     dbp = _vec(db, "db", dt, dev, n)
     _bind_stream(ctx)
     _check("mlp_linear_backward",
-           load().mlp_linear_backward(ctx.handle, xp, ldx, zp, ldz, gyp, lddy, rows, float(p), gp, dxp,
-                                      lddx, dwp, dbp))
+           load().mlp_linear_backward(ctx.handle, xp, ldx, zp, ldz, gyp, lddy, rows, float(p), gp,
+                                      dxp, lddx, dwp, dbp))
     return dX, dW, db
 
 
 def _dropout_call(fn, X, p, rng, residual, out, name):
     if X.dim() != 2:
         raise ValueError("%s must be [rows, cols]" % name)
-    if X.dtype not in DTYPES:
-        raise TypeError("%s must be one of %s" % (name, tuple(DTYPES)))
-    rows, cols = X.shape
     dev, dt = X.device, X.dtype
+    if dt not in DTYPES:
+        raise TypeError("%s must be one of %s" % (name, tuple(DTYPES)))
+    if not X.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    rows, cols = X.shape
     xp, ldx = _mat(X, name, dt, dev, rows, cols)
     rp, ldr = _mat(residual, "residual", dt, dev, rows, cols)
     gp = _rng(rng, dev)
+    p = float(p)
     if out is None:
-        out = torch.empty(rows, cols, dtype=dt, device=dev)
-    yp, ldy = _mat(out, "out", dt, dev, rows, cols)
-    args = (xp, ldx, float(p), gp, yp, ldy)
+        out = torch.empty((rows, cols), dtype=dt, device=dev)
+        yp, ldy = out.data_ptr(), cols
+    else:
+        yp, ldy = _mat(out, "out", dt, dev, rows, cols)
+    args = (xp, ldx, p, gp, yp, ldy)
     if fn == "mlp_dropout_forward":
-        args = (xp, ldx, rp, ldr, float(p), gp, yp, ldy)
-    f, s = getattr(load(), fn), torch.cuda.current_stream(dev).cuda_stream
+        args = (xp, ldx, rp, ldr, p, gp, yp, ldy)
+    f, s = getattr(load(), fn), _current_stream(dev.index)
     if dev.index == torch.cuda.current_device():
         st = f(DTYPES[dt], rows, cols, *args, s)
     else:
