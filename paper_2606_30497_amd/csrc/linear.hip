@@ -14,6 +14,7 @@ namespace mlp {
 constexpr int64_t LINEAR_MAX_WIDTH = 1 << 20;
 constexpr int COL_CHUNKS = 256;                   // most row chunks of the column sums
 constexpr int64_t ARRIVED_WORDS = 16384;
+constexpr int64_t FEW_ROWS = 2048;                // most rows of a small product (few_rows)
 constexpr int64_t PART_FLOATS_MAX = 256 * 65536;  // 256 workgroups' tiles of partial sums
 
 struct LinearCtx {
@@ -23,7 +24,7 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     uint16_t *g = nullptr, *x = nullptr, *w = nullptr;
-    uint16_t *g_few = nullptr;  // fp32: the parts of g where g itself is fp32 (up to 64 rows)
+    uint16_t *g_few = nullptr;  // fp32: the parts of g where g itself is fp32 (up to FEW_ROWS rows)
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
@@ -93,16 +94,28 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
     if (a.drop.rng) st.init(a.drop, a.N);
     float sum[8] = {};
     if (c < a.N) {
-        for (int64_t r = r0 + t / a.groups; r < r1; r += 256 / a.groups) {
-            float v[8];
-            load8((const T *)a.dY + r * a.lddy, c, a.N, v);
-            if (a.act != MLP_ACT_NONE) {
-                float z[8];
-                load8((const T *)a.Z + r * a.ldz, c, a.N, z);
-                activate_back8(a.act, z, v);
+        const int64_t step = 256 / a.groups;
+        int64_t r = r0 + t / a.groups;
+        const T *dY = (const T *)a.dY + r * a.lddy, *Z = (const T *)a.Z + r * a.ldz;
+        Oct<T> dy, z;
+        auto fetch = [&]() __attribute__((always_inline)) {
+            dy = fetch8(dY, c, a.N);
+            if (a.act != MLP_ACT_NONE) z = fetch8(Z, c, a.N);
+            dY += step * a.lddy;
+            Z += step * a.ldz;
+        };
+        if (r < r1) fetch();
+        for (; r < r1; r += step) {
+            float v[8], zf[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = up(dy.e[j]);
+                zf[j] = up(z.e[j]);
             }
+            if (r + step < r1) fetch();   // the next row's, ahead of this one's work
+            if (a.act != MLP_ACT_NONE) activate_back8(a.act, zf, v);
             if (a.drop.rng) drop8(st.bits(r, c), a.drop.threshold, a.drop.scale, v);
-            if (c + 8 > a.N) {   // what pads a row is 0 (a'(0) dropped or not is not)
+            if (c + 8 > a.N) {   // what pads a row is 0
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = c + j < a.N ? v[j] : 0.0f;
             }
@@ -188,7 +201,7 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const size_t element = c->dtype == MLP_F32 ? 6 : 2;
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
     c->g = (uint16_t *)take(element * M * pad8(N));
-    c->g_few = (uint16_t *)take(c->dtype == MLP_F32 ? element * 64 * pad8(N) : 0);
+    c->g_few = (uint16_t *)take(c->dtype == MLP_F32 ? element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N) : 0);
     c->x = (uint16_t *)take(element * M * pad8(K));
     c->w = (uint16_t *)take(element * K * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
@@ -219,10 +232,15 @@ static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t
     return hipGetLastError();
 }
 
-// Whether the products of M rows go to linear_skinny.hip: those of a few rows, and in
-// fp32, where the tiles' operands would be packed first, small ones.
+// Whether the products of M rows go to linear_skinny.hip: those of a few rows, and small
+// ones (us here and on tiles, bf16: 512 x 512 x 512 7.0 and 9.1, 256 x 1,024 x 1,024 7.9 and
+// 11.6, 333 x 776 x 1,000 8.5 and 10.6, 8,192 x 256 x 256 9.2 and 7.7; fp32, whose tiles'
+// operands are packed first: 128 x 1,024 x 1,024 10 and 21, 64 x 4,096 x 4,096 34 and 65,
+// 512 x 1,024 x 1,024 27 and 32).
 static bool few_rows(const LinearCtx &c, int64_t M) {
-    return M <= 32 || (c.dtype == MLP_F32 && (M <= 64 || M * c.d_in * c.d_out <= (1 << 27)));
+    if (c.d_in < SKINNY_WIDTH || c.d_out < SKINNY_WIDTH) return false;
+    const int64_t small = c.dtype == MLP_F32 ? 1 << 29 : 1 << 28;
+    return M <= (c.dtype == MLP_F32 ? 64 : 32) || (M <= FEW_ROWS && M * c.d_in * c.d_out <= small);
 }
 
 template <class T>
@@ -257,8 +275,10 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
         GradArgs a;
+        // few rows: as many rows at a time as there are, and fewer columns
+        const int most = M > 32 && M <= 64 ? 4 : M > 16 && M <= 32 ? 8 : M > 8 && M <= 16 ? 16 : 32;
         a.groups = 1;
-        while (a.groups < 32 && a.groups * 8 < N) a.groups *= 2;
+        while (a.groups < most && a.groups * 8 < N) a.groups *= 2;
         const int64_t step = 256 / a.groups;
         // about four workgroups a compute unit; few rows in one chunk, which gives db
         const int64_t want = ceil_div(1024, ceil_div(N, 8 * a.groups));
@@ -296,11 +316,13 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
             if (hipError_t s = launch_skinny(GEMM_NT, c.dtype, G, ldg, c.W, N, M, K, N, e, c.part,
                                              c.part_floats, c.arrived, c.arrived_words, c.stream))
                 return s;
-        // (fp32 dW of 64 x 4,096 x 4,096: 59 us here, 37 on tiles, parts and all; of 128 x
-        // 1,024 x 1,024 10 us and 16)
-        if (!b.dW || M <= 32 || M * K * N <= (1 << 27))
-            return b.dW ? launch_outer(c.dtype, b.X, b.ldx, G, ldg, M, K, N, b.dW, c.stream) : hipSuccess;
-        if (hipError_t s = operand<T>(c, G, ldg, M, N, c.g_few, &g)) return s;
+        // (dW, us here and on tiles: bf16 256 x 1,024 x 1,024 7.5 and 14.4, 512 x 512 x 512 11.0
+        // and 9.0, 2,000 x 64 x 64 126 and 9.5; fp32 64 x 4,096 x 4,096 59 and 37)
+        if (!b.dW) return hipSuccess;
+        if (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)))
+            return launch_outer(c.dtype, b.X, b.ldx, G, ldg, M, K, N, b.dW, c.stream);
+        if (sizeof(T) == 4 || same)
+            if (hipError_t s = operand<T>(c, G, ldg, M, N, sizeof(T) == 4 ? c.g_few : c.g, &g)) return s;
     }
     if (b.dX && !few) {
         Operand w;

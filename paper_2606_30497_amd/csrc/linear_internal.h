@@ -80,11 +80,13 @@ hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B
 // The products of few rows, or small ones (linear_skinny.hip), on operands as the caller
 // has them, of any alignment. GEMM_NN: Y = X W with W [K x N]; GEMM_NT: W [N x K].
 // part: room for part_floats partial sums; arrived: arrived_words words, zero before the
-// call and after it. The grid is ceil(M / 16 or 32) workgroups high (below 65,536).
+// call and after it. The grid is ceil(M / 16 or 32) workgroups high (below 65,536). N and
+// K are at least SKINNY_WIDTH.
+constexpr int64_t SKINNY_WIDTH = 8;
 hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t ldw,
                          int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part, int64_t part_floats,
                          uint32_t *arrived, int64_t arrived_words, hipStream_t stream);
-// dW [K x N] = X^T G of M rows
+// dW [K x N] = X^T G of M rows, N >= SKINNY_WIDTH
 hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t M,
                         int64_t K, int64_t N, void *dW, hipStream_t stream);
 

@@ -63,63 +63,59 @@ struct Step {
     static __device__ __forceinline__ u4v piece(const char *p, uint32_t off) {
         return reinterpret_cast<const Piece<T> *>(p + off)->get();
     }
-    // PER elements from p + off on, of which n >= 1 are inside; those past them are read
-    // from the last one and, if `zero`, set to 0
-    static __device__ __forceinline__ u4v edge(const char *p, uint32_t off, int n, bool zero) {
-        union {
-            T e[PER];
-            u4v v;
-        } o;
+    // elements [at, at + PER) of a row of `len` >= PER, its first at row + off, those past
+    // its end 0: its last PER elements moved down, so that one load at a valid address does
+    static __device__ __forceinline__ u4v end_piece(const char *row, uint32_t off, int at, int len) {
+        const int from = at < len - PER ? at : len - PER, d = (at - from < PER ? at - from : PER) * (int)sizeof(T);
+        u4v v = piece(row, off + (uint32_t)(from * (int)sizeof(T)));
+        if (sizeof(T) == 2) {   // by bytes: 2, 4, 8, 16
+            const uint32_t up[4] = {v[1], v[2], v[3], 0};
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const T e = *reinterpret_cast<const T *>(p + (off + (uint32_t)(j < n ? j : n - 1) * (uint32_t)sizeof(T)));
-            o.e[j] = zero && j >= n ? (T)0.0f : e;
+            for (int i = 0; i < 4; ++i) v[i] = d & 2 ? __builtin_amdgcn_alignbit(up[i], v[i], 16) : v[i];
         }
-        return o.v;
+        v = d & 4 ? u4v{v[1], v[2], v[3], 0} : v;
+        v = d & 8 ? u4v{v[2], v[3], 0, 0} : v;
+        return d & 16 ? u4v{0, 0, 0, 0} : v;
     }
     // The step at depth k0 (uniform) of the outputs from n0 on. EDGE: the tile reaches past
-    // the outputs; TAIL: the step reaches past the depth. What lies outside is read from
-    // the last row or column inside; past the depth it counts as 0.
+    // the outputs (what is computed of those is not used); TAIL: the step reaches past the
+    // depth, where W and X count as 0.
     template <bool EDGE, bool TAIL>
     __device__ __forceinline__ void load(const void *W, int64_t ld, int64_t N, int64_t depth_all, int64_t n0, int64_t k0) {
         const int l = threadIdx.x & 63, r = l & 15, g = l >> 4;
         const uint32_t ES = sizeof(T), ldw = (uint32_t)ld * ES;
-        const int nl = (int)(N - n0 < SKINNY_N ? N - n0 : SKINNY_N);   // outputs of the tile
-        const int kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);                 // depth of the step
-        const char *base = (const char *)W + (OUT ? k0 * ld + n0 : n0 * ld + k0) * ES;
+        const int kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);   // depth of the step
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if constexpr (OUT) {
                 const int kd = sizeof(T) == 2 ? i : i / 2, k = PER * g + kd;
                 const int n = 8 * r + (sizeof(T) == 2 ? 0 : 4 * (i & 1));
-                const char *row = base;
+                const char *row = (const char *)W + k0 * ld * ES;
                 uint32_t off = (uint32_t)(PER * g) * ldw;
                 if constexpr (TAIL) off = (uint32_t)(k < kl ? k : kl - 1) * ldw;
                 else row += kd * (int64_t)ldw;
-                if constexpr (EDGE) {
-                    const int at = n < nl ? n : nl - 1;
-                    w[i] = edge(row, off + at * ES, nl - at, false);
-                } else {
-                    w[i] = piece(row, off + n * ES);
-                }
+                if constexpr (EDGE) w[i] = end_piece(row, off, (int)n0 + n, (int)N);
+                else w[i] = piece(row + n0 * ES, off + n * ES);
                 if (TAIL && k >= kl) w[i] = u4v{0, 0, 0, 0};
             } else {
-                const char *row = base;
+                const char *row = (const char *)W + n0 * ld * ES;
                 uint32_t off = (uint32_t)(8 * r) * ldw;
-                if constexpr (EDGE) off = (uint32_t)(8 * r + i < nl ? 8 * r + i : nl - 1) * ldw;
+                if constexpr (EDGE) off = (uint32_t)(n0 + 8 * r + i < N ? 8 * r + i : (int)(N - n0) - 1) * ldw;
                 else row += i * (int64_t)ldw;
-                w[i] = TAIL ? depth(row + off, PER * g, kl) : piece(row, off + PER * g * ES);
+                if constexpr (TAIL) w[i] = end_piece(row, off, (int)k0 + PER * g, (int)depth_all);
+                else w[i] = piece(row + k0 * ES, off + PER * g * ES);
             }
         }
     }
     // X's rows at xp (one for each 16 rows), k contiguous
     template <bool TAIL>
     __device__ __forceinline__ void load_x(const char *const (&xp)[MT], int64_t depth_all, int64_t k0) {
-        const int g = (threadIdx.x & 63) >> 4, kl = (int)(depth_all - k0 < K ? depth_all - k0 : K);
+        const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-            x[t] = TAIL ? depth(xp[t] + k0 * (int64_t)sizeof(T), PER * g, kl)
-                        : piece(xp[t] + k0 * (int64_t)sizeof(T), PER * g * (uint32_t)sizeof(T));
+        for (int t = 0; t < MT; ++t) {
+            if constexpr (TAIL) x[t] = end_piece(xp[t], 0, (int)k0 + PER * g, (int)depth_all);
+            else x[t] = piece(xp[t] + k0 * (int64_t)sizeof(T), PER * g * (uint32_t)sizeof(T));
+        }
     }
     // X's columns at xp, k down them, `pitch` bytes apart
     template <bool TAIL>
@@ -140,12 +136,6 @@ struct Step {
             }
             x[t] = o.v;
         }
-    }
-    // elements [k, k + PER) of a row of kl >= 1, those past its end 0
-    static __device__ __forceinline__ u4v depth(const char *row, int k, int kl) {
-        const int at = k < kl ? k : kl - 1;
-        const u4v v = edge(row, (uint32_t)(at * (int)sizeof(T)), kl - at, true);
-        return k < kl ? v : u4v{0, 0, 0, 0};
     }
     __device__ __forceinline__ void multiply(f4 (&acc)[MT][8]) const {
 #pragma unroll
@@ -188,14 +178,7 @@ __device__ __forceinline__ void skinny_sums(const SkinnyArgs &a, int64_t m0, int
         s.template load<EDGE, false>(a.W, a.ldw, a.N, a.K, n0, k0);
         s.template load_x<false>(xp, a.K, k0);
     };
-    if constexpr (EDGE) {
-        S s;
-#pragma unroll 1
-        for (int i = 0; i < full; ++i) {
-            load(s, i);
-            s.multiply(acc);
-        }
-    } else {
+    {
         S s[2];
         if (full > 0) load(s[0], 0);
         if (full > 1) load(s[1], 1);
@@ -305,10 +288,12 @@ template <class T, bool OUT, int MT>
 static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
     constexpr int64_t STEP = Step<T, OUT, MT>::K;
     const int64_t tiles = ceil_div(a.N, SKINNY_N), row_tiles = ceil_div(a.M, 16 * MT), pitch = tiles * SKINNY_N;
-    // A workgroup for each compute unit, of at least two steps a wave. (With 512 of them
+    // A workgroup for each compute unit, of at least two steps a wave (one, where the
+    // workgroups are fewer all the same). (With 512 of them
     // half wait for the other half, whose eight waves' registers fill the unit: fp32 1 x
     // 4,096 x 4,096 16 us with 256, 22 with 512, 20 with 128.)
-    int64_t splits = ceil_div(a.K, 2 * STEP * 8);
+    const int64_t most = ceil_div(a.K, STEP * 8);
+    int64_t splits = tiles * row_tiles * most <= 256 ? most : ceil_div(a.K, 2 * STEP * 8);
     if (splits > 256 / (tiles * row_tiles)) splits = 256 / (tiles * row_tiles);
     if (splits > part_floats / (a.M * pitch)) splits = part_floats / (a.M * pitch);
     if (splits < 1 || tiles * row_tiles > arrived_words) splits = 1;
@@ -321,7 +306,12 @@ static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_word
 
 template <class T, bool OUT>
 static hipError_t skinny_rows(const SkinnyArgs &a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
-    if (a.M <= 16) return skinny<T, OUT, 1>(a, part_floats, arrived_words, stream);
+    // 16 rows a workgroup, and W read again for every 16 (from the caches: 24 x 8,192 x
+    // 2,048 in bf16 12.0 us so, 17.5 with 32 rows), but 32 where W is too large for that or
+    // the workgroups are more than enough
+    if (a.M <= 16 || (a.N * a.K * (int64_t)sizeof(T) <= (32 << 20) &&
+                      ceil_div(a.M, 16) * ceil_div(a.N, SKINNY_N) <= 256))
+        return skinny<T, OUT, 1>(a, part_floats, arrived_words, stream);
     return skinny<T, OUT, 2>(a, part_floats, arrived_words, stream);
 }
 
@@ -387,7 +377,6 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0
             }
         } else {
             int64_t m = 0;
-#pragma unroll 2
             for (; m + S::K <= a.M; m += S::K) {
                 s.template load<EDGE, false>(a.G, a.ldg, a.N, a.M, n0, m);
                 s.template load_across<false>(xp, pitch, a.M, m);
