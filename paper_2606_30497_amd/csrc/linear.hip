@@ -24,7 +24,9 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     uint16_t *g = nullptr, *x = nullptr, *w = nullptr;
-    uint16_t *g_few = nullptr;  // fp32: the parts of g where g itself is fp32 (up to FEW_ROWS rows)
+    // small products (up to FEW_ROWS rows): what the rounding of g to a 16-bit type left;
+    // of an fp32 layer, whose g is fp32 there, its parts
+    uint16_t *g_few = nullptr;
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
@@ -75,6 +77,7 @@ struct GradArgs {
     const void *Z, *dY;
     uint16_t *G;              // nullable, an operand of rows of pad8(N)
     bool parts;               // of an fp32 layer: G in its three parts, else as fp32
+    uint16_t *low;            // nullable: what the rounding of G to a 16-bit type left
     float *col;               // nullable [chunks x N]
     void *db;                 // nullable [N], of a single chunk
     int64_t ldz, lddy, plane, M, N, chunk;   // chunk: rows of a workgroup
@@ -122,6 +125,12 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
             if (a.G) {
                 if (sizeof(T) == 2 || a.parts) put8<T>(a.G + r * ldg + c, a.plane, v);
                 else store8((T *)a.G + r * ldg, c, ldg, v);
+                if (a.low) {
+                    float w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
+                    put8<T>(a.low + r * ldg + c, 0, w);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -201,7 +210,7 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const size_t element = c->dtype == MLP_F32 ? 6 : 2;
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
     c->g = (uint16_t *)take(element * M * pad8(N));
-    c->g_few = (uint16_t *)take(c->dtype == MLP_F32 ? element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N) : 0);
+    c->g_few = (uint16_t *)take(element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N));
     c->x = (uint16_t *)take(element * M * pad8(K));
     c->w = (uint16_t *)take(element * K * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
@@ -246,7 +255,7 @@ static bool few_rows(const LinearCtx &c, int64_t M) {
 template <class T>
 static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx, int64_t rows, const Epilogue &e) {
     if (few_rows(c, rows))
-        return launch_skinny(GEMM_NN, c.dtype, X, ldx, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
+        return launch_skinny(GEMM_NN, c.dtype, X, ldx, 0, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
                              c.part_floats, c.arrived, c.arrived_words, c.stream);
     Operand x, w;
     if (hipError_t s = operand<T>(c, X, ldx, rows, c.d_in, c.x, &x)) return s;
@@ -288,6 +297,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.dY = b.dY;
         a.G = products && !same ? c.g : nullptr;
         a.parts = !few;
+        a.low = sizeof(T) == 2 && few && a.G ? c.g_few : nullptr;
         a.col = b.db && chunks > 1 ? c.col : nullptr;
         a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
@@ -310,17 +320,20 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     if (few) {
         const void *G = same ? b.dY : c.g;
         const int64_t ldg = same ? b.lddy : pad8(N);
+        // The tiles take g rounded to a 16-bit type, once more than its result; here, where
+        // few terms would show it and W or latency is the bound, the rest goes along.
+        const int64_t low = sizeof(T) == 2 && !same ? c.g_few - c.g : 0;
         e.Y = b.dX;
         e.ldy = b.lddx;
         if (b.dX && M > 0)
-            if (hipError_t s = launch_skinny(GEMM_NT, c.dtype, G, ldg, c.W, N, M, K, N, e, c.part,
+            if (hipError_t s = launch_skinny(GEMM_NT, c.dtype, G, ldg, low, c.W, N, M, K, N, e, c.part,
                                              c.part_floats, c.arrived, c.arrived_words, c.stream))
                 return s;
         // (dW, us here and on tiles: bf16 256 x 1,024 x 1,024 7.5 and 14.4, 512 x 512 x 512 11.0
         // and 9.0, 2,000 x 64 x 64 126 and 9.5; fp32 64 x 4,096 x 4,096 59 and 37)
         if (!b.dW) return hipSuccess;
         if (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)))
-            return launch_outer(c.dtype, b.X, b.ldx, G, ldg, M, K, N, b.dW, c.stream);
+            return launch_outer(c.dtype, b.X, b.ldx, G, ldg, low, M, K, N, b.dW, c.stream);
         if (sizeof(T) == 4 || same)
             if (hipError_t s = operand<T>(c, G, ldg, M, N, sizeof(T) == 4 ? c.g_few : c.g, &g)) return s;
     }

@@ -79,16 +79,18 @@ hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B
 
 // The products of few rows, or small ones (linear_skinny.hip), on operands as the caller
 // has them, of any alignment. GEMM_NN: Y = X W with W [K x N]; GEMM_NT: W [N x K].
+// low (GEMM_NT of 16-bit types): 0, or X + low holds what the rounding of X's elements
+// left, and X counts as the sum of both.
 // part: room for part_floats partial sums; arrived: arrived_words words, zero before the
 // call and after it. The grid is ceil(M / 16 or 32) workgroups high (below 65,536). N and
 // K are at least SKINNY_WIDTH.
 constexpr int64_t SKINNY_WIDTH = 8;
-hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t ldw,
-                         int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part, int64_t part_floats,
-                         uint32_t *arrived, int64_t arrived_words, hipStream_t stream);
-// dW [K x N] = X^T G of M rows, N >= SKINNY_WIDTH
-hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t M,
-                        int64_t K, int64_t N, void *dW, hipStream_t stream);
+hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, int64_t low, const void *W,
+                         int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part,
+                         int64_t part_floats, uint32_t *arrived, int64_t arrived_words, hipStream_t stream);
+// dW [K x N] = X^T G of M rows, N >= SKINNY_WIDTH; low as above, of G
+hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t low,
+                        int64_t M, int64_t K, int64_t N, void *dW, hipStream_t stream);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -30,6 +30,7 @@ constexpr int SKINNY_N = 128;   // outputs of a workgroup
 
 struct SkinnyArgs {
     const void *X, *W;
+    int64_t low;           // LOW: elements from X to what its rounding left (the same ld)
     int64_t ldx, ldw, M, N, K;
     int splits;
     int64_t kw;            // depth of a wave (a multiple of the step)
@@ -55,10 +56,11 @@ struct __attribute__((packed, aligned(sizeof(T)))) Piece {
 // 16-bit: w[i] = outputs 8 r .. + 7 of k 8 g + i (OUT: W's rows lie along the outputs), or k
 // 8 g .. + 7 of output 8 r + i. fp32: w[2 s + h] = outputs 8 r + 4 h .. + 3 of k 4 g + s, or
 // w[i] = k 4 g .. + 3 of output 8 r + i. (Lane l: r = l % 16, g = l / 16.)
-template <class T, bool OUT, int MT>
+// LOW: X comes as two values of the type, the second what the first one's rounding left.
+template <class T, bool OUT, int MT, bool LOW = false>
 struct Step {
     static constexpr int PER = 16 / sizeof(T), K = 4 * PER;   // elements of a piece, depth
-    u4v w[8], x[MT];
+    u4v w[8], x[MT], y[LOW ? MT : 1];   // y: X's second values
 
     static __device__ __forceinline__ u4v piece(const char *p, uint32_t off) {
         return reinterpret_cast<const Piece<T> *>(p + off)->get();
@@ -109,12 +111,16 @@ struct Step {
     }
     // X's rows at xp (one for each 16 rows), k contiguous
     template <bool TAIL>
-    __device__ __forceinline__ void load_x(const char *const (&xp)[MT], int64_t depth_all, int64_t k0) {
+    __device__ __forceinline__ void load_x(const char *const (&xp)[MT], int64_t low, int64_t depth_all, int64_t k0) {
         const int g = (threadIdx.x & 63) >> 4;
+        auto get = [&](const char *p) __attribute__((always_inline)) {
+            if constexpr (TAIL) return end_piece(p, 0, (int)k0 + PER * g, (int)depth_all);
+            else return piece(p + k0 * (int64_t)sizeof(T), PER * g * (uint32_t)sizeof(T));
+        };
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            if constexpr (TAIL) x[t] = end_piece(xp[t], 0, (int)k0 + PER * g, (int)depth_all);
-            else x[t] = piece(xp[t] + k0 * (int64_t)sizeof(T), PER * g * (uint32_t)sizeof(T));
+            x[t] = get(xp[t]);
+            if constexpr (LOW) y[t] = get(xp[t] + low * (int64_t)sizeof(T));
         }
     }
     // X's columns at xp, k down them, `pitch` bytes apart
@@ -148,7 +154,10 @@ struct Step {
                         f[q] = __builtin_amdgcn_perm(w[2 * q + 1][t >> 1], w[2 * q][t >> 1], t & 1 ? 0x07060302 : 0x05040100);
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) acc[m][t] = mma16<T>(f, x[m], acc[m][t]);
+                for (int m = 0; m < MT; ++m) {
+                    if constexpr (LOW) acc[m][t] = mma16<T>(f, y[m], acc[m][t]);
+                    acc[m][t] = mma16<T>(f, x[m], acc[m][t]);
+                }
             } else {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
@@ -162,9 +171,9 @@ struct Step {
     }
 };
 
-template <class T, bool OUT, int MT, bool EDGE>
+template <class T, bool OUT, int MT, bool LOW, bool EDGE>
 __device__ __forceinline__ void skinny_sums(const SkinnyArgs &a, int64_t m0, int64_t n0, int64_t kb, f4 (&acc)[MT][8]) {
-    typedef Step<T, OUT, MT> S;
+    typedef Step<T, OUT, MT, LOW> S;
     const int64_t ke = kb + a.kw < a.K ? kb + a.kw : a.K;
     const int full = ke > kb ? (int)((ke - kb) / S::K) : 0;
     const char *xp[MT];
@@ -176,7 +185,7 @@ __device__ __forceinline__ void skinny_sums(const SkinnyArgs &a, int64_t m0, int
     auto load = [&](S &s, int i) __attribute__((always_inline)) {
         const int64_t k0 = kb + i * (int64_t)S::K;
         s.template load<EDGE, false>(a.W, a.ldw, a.N, a.K, n0, k0);
-        s.template load_x<false>(xp, a.K, k0);
+        s.template load_x<false>(xp, a.low, a.K, k0);
     };
     {
         S s[2];
@@ -194,12 +203,12 @@ __device__ __forceinline__ void skinny_sums(const SkinnyArgs &a, int64_t m0, int
     if (kb + (int64_t)full * S::K < ke) {
         S s;
         s.template load<EDGE, true>(a.W, a.ldw, a.N, a.K, n0, kb + (int64_t)full * S::K);
-        s.template load_x<true>(xp, a.K, kb + (int64_t)full * S::K);
+        s.template load_x<true>(xp, a.low, a.K, kb + (int64_t)full * S::K);
         s.multiply(acc);
     }
 }
 
-template <class T, bool OUT, int MT>
+template <class T, bool OUT, int MT, bool LOW>
 __global__ __launch_bounds__(512, 2) void k_skinny(const SkinnyArgs a) {
     constexpr int WAVES = 8, NT = 512, CS = SKINNY_N + 4;
     __shared__ __attribute__((aligned(16))) float sums[WAVES][16 * MT][CS];
@@ -214,8 +223,8 @@ __global__ __launch_bounds__(512, 2) void k_skinny(const SkinnyArgs a) {
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int t = 0; t < 8; ++t) acc[m][t] = f4{0.f, 0.f, 0.f, 0.f};
-    if (n0 + SKINNY_N <= a.N) skinny_sums<T, OUT, MT, false>(a, m0, n0, kb, acc);
-    else skinny_sums<T, OUT, MT, true>(a, m0, n0, kb, acc);
+    if (n0 + SKINNY_N <= a.N) skinny_sums<T, OUT, MT, LOW, false>(a, m0, n0, kb, acc);
+    else skinny_sums<T, OUT, MT, LOW, true>(a, m0, n0, kb, acc);
 
     // register v of product t: row l % 16, column 8 (4 (l / 16) + v) + t
 #pragma unroll
@@ -284,7 +293,7 @@ __global__ __launch_bounds__(512, 2) void k_skinny(const SkinnyArgs a) {
     }
 }
 
-template <class T, bool OUT, int MT>
+template <class T, bool OUT, int MT, bool LOW>
 static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
     constexpr int64_t STEP = Step<T, OUT, MT>::K;
     const int64_t tiles = ceil_div(a.N, SKINNY_N), row_tiles = ceil_div(a.M, 16 * MT), pitch = tiles * SKINNY_N;
@@ -299,32 +308,40 @@ static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_word
     if (splits < 1 || tiles * row_tiles > arrived_words) splits = 1;
     a.kw = ceil_div(ceil_div(a.K, splits * 8), STEP) * STEP;
     a.splits = (int)ceil_div(a.K, a.kw * 8);
-    hipLaunchKernelGGL((k_skinny<T, OUT, MT>), dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles), dim3(512), 0,
+    hipLaunchKernelGGL((k_skinny<T, OUT, MT, LOW>), dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles), dim3(512), 0,
                        stream, a);
     return hipGetLastError();
 }
 
-template <class T, bool OUT>
+template <class T, bool OUT, bool LOW = false>
 static hipError_t skinny_rows(const SkinnyArgs &a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
     // 16 rows a workgroup, and W read again for every 16 (from the caches: 24 x 8,192 x
     // 2,048 in bf16 12.0 us so, 17.5 with 32 rows), but 32 where W is too large for that or
     // the workgroups are more than enough
     if (a.M <= 16 || (a.N * a.K * (int64_t)sizeof(T) <= (32 << 20) &&
                       ceil_div(a.M, 16) * ceil_div(a.N, SKINNY_N) <= 256))
-        return skinny<T, OUT, 1>(a, part_floats, arrived_words, stream);
-    return skinny<T, OUT, 2>(a, part_floats, arrived_words, stream);
+        return skinny<T, OUT, 1, LOW>(a, part_floats, arrived_words, stream);
+    return skinny<T, OUT, 2, LOW>(a, part_floats, arrived_words, stream);
 }
 
-hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t ldw,
-                         int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part, int64_t part_floats,
-                         uint32_t *arrived, int64_t arrived_words, hipStream_t stream) {
-    const SkinnyArgs a{X, W, ldx, ldw, M, N, K, 1, 0, part, arrived, e};
-    const bool out = op == GEMM_NN;
-#define SKINNY(T) \
-    (out ? skinny_rows<T, true>(a, part_floats, arrived_words, stream) \
-         : skinny_rows<T, false>(a, part_floats, arrived_words, stream))
-    return dtype == MLP_F32 ? SKINNY(float) : dtype == MLP_BF16 ? SKINNY(bf16) : SKINNY(f16);
-#undef SKINNY
+template <class T>
+static hipError_t skinny_type(int op, const SkinnyArgs &a, int64_t part_floats, int64_t arrived_words,
+                              hipStream_t stream) {
+    if (op == GEMM_NN) return skinny_rows<T, true>(a, part_floats, arrived_words, stream);
+    if constexpr (sizeof(T) == 2)
+        if (a.low) return skinny_rows<T, false, true>(a, part_floats, arrived_words, stream);
+    return skinny_rows<T, false>(a, part_floats, arrived_words, stream);
+}
+
+hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, int64_t low, const void *W,
+                         int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part,
+                         int64_t part_floats, uint32_t *arrived, int64_t arrived_words, hipStream_t stream) {
+    const SkinnyArgs a{X, W, low, ldx, ldw, M, N, K, 1, 0, part, arrived, e};
+    switch (dtype) {
+    case MLP_F32: return skinny_type<float>(op, a, part_floats, arrived_words, stream);
+    case MLP_BF16: return skinny_type<bf16>(op, a, part_floats, arrived_words, stream);
+    default: return skinny_type<f16>(op, a, part_floats, arrived_words, stream);
+    }
 }
 
 // Element v of lane group g (of 16 lanes) and element g of group v change places.
@@ -351,18 +368,23 @@ __device__ __forceinline__ void trade(f4 &x) {
 struct OuterArgs {
     const void *X, *G;
     void *dW;
+    int64_t low;   // LOW: elements from G to what its rounding left
     int64_t ldx, ldg, M, K, N;
-    int tiles;   // tiles of 16 k a wave
+    int tiles;     // tiles of 16 k a wave
 };
 
-template <class T, bool EDGE>
+template <class T, bool LOW, bool EDGE>
 __device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0) {
     typedef Step<T, true, 1> S;
     const int lane = threadIdx.x & 63;
     const int64_t pitch = a.ldx * (int64_t)sizeof(T);
+    const T *low = (const T *)a.G + a.low;
     const bool once = a.M <= S::K;   // G's rows stay in the registers for all tiles
-    S s;
-    if (once && a.M > 0) s.template load<EDGE, true>(a.G, a.ldg, a.N, a.M, n0, 0);
+    S s, y;                          // y: the second values of G
+    if (once && a.M > 0) {
+        s.template load<EDGE, true>(a.G, a.ldg, a.N, a.M, n0, 0);
+        if constexpr (LOW) y.template load<EDGE, true>(low, a.ldg, a.N, a.M, n0, 0);
+    }
 #pragma unroll 1
     for (int i = 0; i < a.tiles && k0 < a.K; ++i, k0 += 16) {
         const int64_t k = k0 + (lane & 15);
@@ -370,24 +392,21 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0
         f4 acc[1][8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) acc[0][t] = f4{0.f, 0.f, 0.f, 0.f};
-        if (once) {
-            if (a.M > 0) {
-                s.template load_across<true>(xp, pitch, a.M, 0);
-                s.multiply(acc);
+        auto product = [&](auto tail, int64_t m) __attribute__((always_inline)) {
+            constexpr bool TAIL = decltype(tail)::value;
+            s.template load_across<TAIL>(xp, pitch, a.M, m);
+            if constexpr (LOW) {
+                if (!once) y.template load<EDGE, TAIL>(low, a.ldg, a.N, a.M, n0, m);
+                y.x[0] = s.x[0];
+                y.multiply(acc);
             }
-        } else {
-            int64_t m = 0;
-            for (; m + S::K <= a.M; m += S::K) {
-                s.template load<EDGE, false>(a.G, a.ldg, a.N, a.M, n0, m);
-                s.template load_across<false>(xp, pitch, a.M, m);
-                s.multiply(acc);
-            }
-            if (m < a.M) {
-                s.template load<EDGE, true>(a.G, a.ldg, a.N, a.M, n0, m);
-                s.template load_across<true>(xp, pitch, a.M, m);
-                s.multiply(acc);
-            }
-        }
+            if (!once) s.template load<EDGE, TAIL>(a.G, a.ldg, a.N, a.M, n0, m);
+            s.multiply(acc);
+        };
+        int64_t m = 0;
+        if (!once)
+            for (; m + S::K <= a.M; m += S::K) product(std::false_type(), m);
+        if (m < a.M) product(std::true_type(), m);
         // Register v of lane group g is piece 4 g + v of the row: traded among the four
         // groups, piece 4 v + g, so that a store's four lanes of a row write side by side.
 #pragma unroll
@@ -405,25 +424,33 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0
     }
 }
 
-template <class T>
+template <class T, bool LOW>
 __global__ __launch_bounds__(256) void k_outer(const OuterArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = (int64_t)blockIdx.x * SKINNY_N, k0 = ((int64_t)blockIdx.y * 4 + wave) * (16 * a.tiles);
-    if (n0 + SKINNY_N <= a.N) outer<T, false>(a, k0, n0);
-    else outer<T, true>(a, k0, n0);
+    if (n0 + SKINNY_N <= a.N) outer<T, LOW, false>(a, k0, n0);
+    else outer<T, LOW, true>(a, k0, n0);
 }
 
-hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t M,
-                        int64_t K, int64_t N, void *dW, hipStream_t stream) {
+hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t low,
+                        int64_t M, int64_t K, int64_t N, void *dW, hipStream_t stream) {
     // about 1,024 workgroups of four waves
     const int64_t across = ceil_div(N, SKINNY_N), tiles = ceil_div(ceil_div(K, 64) * across, 1024);
-    const OuterArgs a{X, G, dW, ldx, ldg, M, K, N, (int)(tiles < 16 ? tiles : 16)};
+    const OuterArgs a{X, G, dW, low, ldx, ldg, M, K, N, (int)(tiles < 16 ? tiles : 16)};
     const dim3 grid((unsigned)across, (unsigned)ceil_div(K, 64 * a.tiles));
+#define OUTER(T, LOW) hipLaunchKernelGGL((k_outer<T, LOW>), grid, dim3(256), 0, stream, a)
     switch (dtype) {
-    case MLP_F32: hipLaunchKernelGGL(k_outer<float>, grid, dim3(256), 0, stream, a); break;
-    case MLP_BF16: hipLaunchKernelGGL(k_outer<bf16>, grid, dim3(256), 0, stream, a); break;
-    default: hipLaunchKernelGGL(k_outer<f16>, grid, dim3(256), 0, stream, a); break;
+    case MLP_F32: OUTER(float, false); break;
+    case MLP_BF16:
+        if (low) OUTER(bf16, true);
+        else OUTER(bf16, false);
+        break;
+    default:
+        if (low) OUTER(f16, true);
+        else OUTER(f16, false);
+        break;
     }
+#undef OUTER
     return hipGetLastError();
 }
 

@@ -656,6 +656,8 @@ def _dropout_call(fn, X, p, rng, residual, out, name):
     rp, ldr = _mat(residual, "residual", dt, dev, rows, cols)
     gp = _rng(rng, dev)
     p = float(p)
+    if p == 0.0 and out is None and residual is None:
+        return X
     if out is None:
         out = torch.empty((rows, cols), dtype=dt, device=dev)
         yp, ldy = out.data_ptr(), cols
@@ -676,10 +678,12 @@ def _dropout_call(fn, X, p, rng, residual, out, name):
 
 def mlp_dropout_forward(X, p, rng, residual=None, out=None):
     """residual + dropout(X) on the current stream of X's device; rng int64 [2] (seed,
-    offset) in device memory. out may be X or residual."""
+    offset) in device memory. out may be X or residual. With p = 0, no residual and no out
+    the result is X itself."""
     return _dropout_call("mlp_dropout_forward", X, p, rng, residual, out, "X")
 
 
 def mlp_dropout_backward(dY, p, rng, out=None):
-    """The gradient of mlp_dropout_forward with the same p and rng; out may be dY."""
+    """The gradient of mlp_dropout_forward with the same p and rng; out may be dY. With p =
+    0 and no out the result is dY itself."""
     return _dropout_call("mlp_dropout_backward", dY, p, rng, None, out, "dY")
