@@ -23,10 +23,8 @@ struct LinearCtx {
     const void *W = nullptr, *bias = nullptr;
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
-    uint16_t *g = nullptr, *x = nullptr, *w = nullptr;
-    // small products (up to FEW_ROWS rows): what the rounding of g to a 16-bit type left;
-    // of an fp32 layer, whose g is fp32 there, its parts
-    uint16_t *g_few = nullptr;
+    void *g = nullptr, *x = nullptr, *w = nullptr;
+    void *low = nullptr;        // what g's rounding to a 16-bit type left (up to FEW_ROWS rows)
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
@@ -38,36 +36,16 @@ struct LinearCtx {
 
 static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 
-// v as an operand's elements [c, c + 8) of a row: rounded to the 16-bit type, or the
-// three bf16 parts of fp32, `plane` apart
-template <class T>
-__device__ __forceinline__ void put8(uint16_t *p, int64_t plane, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        Oct<T> o;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o.e[j] = (T)v[j];
-        *reinterpret_cast<u4v *>(p) = __builtin_bit_cast(u4v, o);
-    } else {
-        uint32_t w[4][3];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) split_pair(v[2 * j], v[2 * j + 1], w[j]);
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            *reinterpret_cast<u4v *>(p + i * plane) = u4v{w[0][i], w[1][i], w[2][i], w[3][i]};
-    }
-}
-
 // A matrix of rows x cols laid out as an operand: rows of pad8(cols) elements, what pads
-// them zero. Read and written once, bound by memory (fp32: 10 bytes an element).
+// them zero. Read and written once, bound by memory.
 template <class T>
-__global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t rows, int64_t cols, uint16_t *out,
-                                              int64_t plane) {
+__global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t rows, int64_t cols, T *out) {
     const int64_t blocks = (cols + 7) / 8, total = rows * blocks, step = (int64_t)gridDim.x * 256;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
         const int64_t r = i / blocks, c = (i - r * blocks) * 8;
         float v[8];
         load8(P + r * ld, c, cols, v);
-        put8<T>(out + i * 8, plane, v);
+        store8(out + r * blocks * 8, c, blocks * 8, v);
     }
 }
 
@@ -75,12 +53,11 @@ __global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t ro
 // and 8 * groups columns.
 struct GradArgs {
     const void *Z, *dY;
-    uint16_t *G;              // nullable, an operand of rows of pad8(N)
-    bool parts;               // of an fp32 layer: G in its three parts, else as fp32
-    uint16_t *low;            // nullable: what the rounding of G to a 16-bit type left
+    void *G;                  // nullable, an operand of rows of pad8(N)
+    void *low;                // nullable: what the rounding of G to a 16-bit type left
     float *col;               // nullable [chunks x N]
     void *db;                 // nullable [N], of a single chunk
-    int64_t ldz, lddy, plane, M, N, chunk;   // chunk: rows of a workgroup
+    int64_t ldz, lddy, M, N, chunk;   // chunk: rows of a workgroup
     int groups;               // a power of two up to 32
     int act;
     Drop drop;
@@ -122,15 +99,12 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = c + j < a.N ? v[j] : 0.0f;
             }
-            if (a.G) {
-                if (sizeof(T) == 2 || a.parts) put8<T>(a.G + r * ldg + c, a.plane, v);
-                else store8((T *)a.G + r * ldg, c, ldg, v);
-                if (a.low) {
-                    float w[8];
+            if (a.G) store8((T *)a.G + r * ldg, c, ldg, v);
+            if (a.low) {
+                float w[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
-                    put8<T>(a.low + r * ldg + c, 0, w);
-                }
+                for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
+                store8((T *)a.low + r * ldg, c, ldg, w);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -207,12 +181,12 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
         at += pad256(bytes);
         return p;
     };
-    const size_t element = c->dtype == MLP_F32 ? 6 : 2;
+    const size_t element = dtype_bytes(c->dtype);
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
-    c->g = (uint16_t *)take(element * M * pad8(N));
-    c->g_few = (uint16_t *)take(element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N));
-    c->x = (uint16_t *)take(element * M * pad8(K));
-    c->w = (uint16_t *)take(element * K * pad8(N));
+    c->g = take(element * M * pad8(N));
+    c->low = take(element == 2 ? element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N) : 0);
+    c->x = take(element * M * pad8(K));
+    c->w = take(element * K * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
     int64_t most = M * N > M * K ? M * N : M * K;
     if (most < K * N) most = K * N;
@@ -223,21 +197,22 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     return at;
 }
 
-// The matrix [rows x cols] at P as an operand: as it is where its type and layout are an
-// operand's (rows close enough for 32-bit offsets within a tile), else packed at `room`.
+// The matrix [rows x cols] at P as an operand: as it is where its layout is an operand's
+// (and its rows close enough for 32-bit offsets within a tile), else packed at `room`.
 template <class T>
-static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t rows, int64_t cols,
-                          uint16_t *room, Operand *o) {
+static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t rows, int64_t cols, void *room,
+                          Operand *o) {
     if (rows <= 1) ld = pad8(cols);
-    if (sizeof(T) == 2 && ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < (1 << 22)) {
-        *o = Operand{(const uint16_t *)P, ld, 0};
+    const bool fits = sizeof(T) == 4 ? cols >= 4 : ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0;
+    if (fits && ld < (1 << 22)) {
+        *o = Operand{P, ld, cols};
         return hipSuccess;
     }
-    *o = Operand{room, pad8(cols), rows * pad8(cols)};
+    *o = Operand{room, pad8(cols), pad8(cols)};
     if (rows == 0) return hipSuccess;
     const int64_t need = ceil_div(rows * (pad8(cols) / 8), 256);
     hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)(need < 8192 ? need : 8192)), dim3(256), 0, c.stream,
-                       (const T *)P, ld, rows, cols, room, o->plane);
+                       (const T *)P, ld, rows, cols, (T *)room);
     return hipGetLastError();
 }
 
@@ -278,7 +253,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // without activation and dropout g is dY, and dY itself the operand (of few rows, where
     // 32-bit offsets reach over the depth of a step)
     const bool same = c.act == MLP_ACT_NONE && !b.drop.rng && (!few || b.lddy < (1 << 24));
-    Operand g{c.g, pad8(N), M * pad8(N)};
+    Operand g{c.g, pad8(N), pad8(N)};
     if (products && same && !few)
         if (hipError_t e = operand<T>(c, b.dY, b.lddy, M, N, c.g, &g)) return e;
     int64_t chunks = 0;
@@ -296,13 +271,11 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.Z = b.Z;
         a.dY = b.dY;
         a.G = products && !same ? c.g : nullptr;
-        a.parts = !few;
-        a.low = sizeof(T) == 2 && few && a.G ? c.g_few : nullptr;
+        a.low = sizeof(T) == 2 && few && a.G ? c.low : nullptr;
         a.col = b.db && chunks > 1 ? c.col : nullptr;
         a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
         a.lddy = b.lddy;
-        a.plane = g.plane;
         a.M = M;
         a.N = N;
         a.act = c.act;
@@ -322,7 +295,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         const int64_t ldg = same ? b.lddy : pad8(N);
         // The tiles take g rounded to a 16-bit type, once more than its result; here, where
         // few terms would show it and W or latency is the bound, the rest goes along.
-        const int64_t low = sizeof(T) == 2 && !same ? c.g_few - c.g : 0;
+        const int64_t low = sizeof(T) == 2 && !same ? (T *)c.low - (T *)c.g : 0;
         e.Y = b.dX;
         e.ldy = b.lddx;
         if (b.dX && M > 0)
@@ -334,8 +307,8 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         if (!b.dW) return hipSuccess;
         if (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)))
             return launch_outer(c.dtype, b.X, b.ldx, G, ldg, low, M, K, N, b.dW, c.stream);
-        if (sizeof(T) == 4 || same)
-            if (hipError_t s = operand<T>(c, G, ldg, M, N, sizeof(T) == 4 ? c.g_few : c.g, &g)) return s;
+        if (same)
+            if (hipError_t s = operand<T>(c, G, ldg, M, N, c.g, &g)) return s;
     }
     if (b.dX && !few) {
         Operand w;

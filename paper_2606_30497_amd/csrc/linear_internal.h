@@ -50,12 +50,12 @@ struct Finish {
     }
 };
 
-// An operand of a product on the matrix cores, as 16-bit values: rows of `ld` elements,
-// 16-byte aligned, ld and the length of a row multiples of 8 (what pads a row is zero).
-// fp32 operands are three such matrices of bf16 parts (bf16x3.h), `plane` elements apart.
+// An operand of a product on tiles: rows of `ld` elements. 16-bit: 16-byte aligned, ld and
+// the length of a row multiples of 8 (what pads a row is zero). fp32: at any address, `len`
+// elements of a row readable, four at least (what pads a row is zero).
 struct Operand {
-    const uint16_t *p;
-    int64_t ld, plane;
+    const void *p;
+    int64_t ld, len;
 };
 
 // C[m][n] = sum_k a(m, k) b(k, n) for m < M, n < N, k < K. The products there are:
@@ -76,6 +76,11 @@ struct GemmArgs {
 // launches on `stream`.
 hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N,
                        int64_t K, const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream);
+
+hipError_t launch_gemm_f32(int op, const GemmArgs &g, int64_t part_floats, hipStream_t stream);
+// the splits' sums through the epilogue, where there are splits
+template <class T>
+hipError_t join_splits(const GemmArgs &g, hipStream_t stream);
 
 // The products of few rows, or small ones (linear_skinny.hip), on operands as the caller
 // has them, of any alignment. GEMM_NN: Y = X W with W [K x N]; GEMM_NT: W [N x K].
