@@ -24,7 +24,7 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     void *g = nullptr, *x = nullptr, *w = nullptr;
-    void *low = nullptr;        // what g's rounding to a 16-bit type left (up to FEW_ROWS rows)
+    void *low = nullptr;        // what g's rounding to a 16-bit type left (up to 64 rows)
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
@@ -36,12 +36,28 @@ struct LinearCtx {
 
 static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 
-// A matrix of rows x cols laid out as an operand: rows of pad8(cols) elements, what pads
-// them zero. Read and written once, bound by memory.
+// Matrices of rows x cols to be laid out as operands: rows of pad8(cols) elements, what pads
+// them zero. Read and written once, bound by memory; one launch for all of a call's.
+struct PackArgs {
+    struct Job {
+        const void *P;
+        void *out;
+        int64_t ld, rows, cols;
+    } job[3];
+    int64_t groups[3];   // of workgroups, up to and with each job's
+    int jobs;
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void k_pack(const T *P, int64_t ld, int64_t rows, int64_t cols, T *out) {
-    const int64_t blocks = (cols + 7) / 8, total = rows * blocks, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+__global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
+    int j = 0;
+    while (j + 1 < a.jobs && blockIdx.x >= a.groups[j]) ++j;
+    const int64_t first = j ? a.groups[j - 1] : 0, step = (a.groups[j] - first) * 256;
+    const T *P = (const T *)a.job[j].P;
+    T *out = (T *)a.job[j].out;
+    const int64_t ld = a.job[j].ld, cols = a.job[j].cols;
+    const int64_t blocks = (cols + 7) / 8, total = a.job[j].rows * blocks;
+    for (int64_t i = ((int64_t)blockIdx.x - first) * 256 + threadIdx.x; i < total; i += step) {
         const int64_t r = i / blocks, c = (i - r * blocks) * 8;
         float v[8];
         load8(P + r * ld, c, cols, v);
@@ -184,7 +200,7 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const size_t element = dtype_bytes(c->dtype);
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
     c->g = take(element * M * pad8(N));
-    c->low = take(element == 2 ? element * (M < FEW_ROWS ? M : FEW_ROWS) * pad8(N) : 0);
+    c->low = take(element == 2 ? element * (M < 64 ? M : 64) * pad8(N) : 0);
     c->x = take(element * M * pad8(K));
     c->w = take(element * K * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
@@ -197,24 +213,34 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     return at;
 }
 
-// The matrix [rows x cols] at P as an operand: as it is where its layout is an operand's
-// (and its rows close enough for 32-bit offsets within a tile), else packed at `room`.
-template <class T>
-static hipError_t operand(const LinearCtx &c, const void *P, int64_t ld, int64_t rows, int64_t cols, void *room,
-                          Operand *o) {
-    if (rows <= 1) ld = pad8(cols);
-    const bool fits = sizeof(T) == 4 ? cols >= 4 : ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0;
-    if (fits && ld < (1 << 22)) {
-        *o = Operand{P, ld, cols};
-        return hipSuccess;
+// Operands of a call's products.
+struct Operands {
+    const LinearCtx &c;
+    PackArgs a{};
+    explicit Operands(const LinearCtx &ctx) : c(ctx) {}
+    // The matrix [rows x cols] at P: as it is where its layout is an operand's (and its rows
+    // close enough for 32-bit offsets within a tile), else packed at `room` by launch().
+    template <class T>
+    Operand get(const void *P, int64_t ld, int64_t rows, int64_t cols, void *room) {
+        if (rows <= 1) ld = pad8(cols);
+        const bool fits = sizeof(T) == 4 ? cols >= 4 : ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0;
+        if (fits && ld < (1 << 22)) return Operand{P, ld, cols};
+        if (rows > 0) {
+            const int64_t need = ceil_div(rows * (pad8(cols) / 8), 256);
+            a.job[a.jobs] = PackArgs::Job{P, room, ld, rows, cols};
+            a.groups[a.jobs] = (a.jobs ? a.groups[a.jobs - 1] : 0) + (need < 4096 ? need : 4096);
+            ++a.jobs;
+        }
+        return Operand{room, pad8(cols), pad8(cols)};
     }
-    *o = Operand{room, pad8(cols), pad8(cols)};
-    if (rows == 0) return hipSuccess;
-    const int64_t need = ceil_div(rows * (pad8(cols) / 8), 256);
-    hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)(need < 8192 ? need : 8192)), dim3(256), 0, c.stream,
-                       (const T *)P, ld, rows, cols, (T *)room);
-    return hipGetLastError();
-}
+    template <class T>
+    hipError_t launch() {
+        if (a.jobs == 0) return hipSuccess;
+        hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)a.groups[a.jobs - 1]), dim3(256), 0, c.stream, a);
+        a.jobs = 0;
+        return hipGetLastError();
+    }
+};
 
 // Whether the products of M rows go to linear_skinny.hip: those of a few rows, and small
 // ones (us here and on tiles, bf16: 512 x 512 x 512 7.0 and 9.1, 256 x 1,024 x 1,024 7.9 and
@@ -232,9 +258,9 @@ static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx,
     if (few_rows(c, rows))
         return launch_skinny(GEMM_NN, c.dtype, X, ldx, 0, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
                              c.part_floats, c.arrived, c.arrived_words, c.stream);
-    Operand x, w;
-    if (hipError_t s = operand<T>(c, X, ldx, rows, c.d_in, c.x, &x)) return s;
-    if (hipError_t s = operand<T>(c, c.W, c.d_out, c.d_in, c.d_out, c.w, &w)) return s;
+    Operands o(c);
+    const Operand x = o.get<T>(X, ldx, rows, c.d_in, c.x), w = o.get<T>(c.W, c.d_out, c.d_in, c.d_out, c.w);
+    if (hipError_t s = o.launch<T>()) return s;
     return launch_gemm(GEMM_NN, c.dtype, x, w, rows, c.d_out, c.d_in, e, c.part, c.part_floats, c.stream);
 }
 
@@ -253,9 +279,26 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // without activation and dropout g is dY, and dY itself the operand (of few rows, where
     // 32-bit offsets reach over the depth of a step)
     const bool same = c.act == MLP_ACT_NONE && !b.drop.rng && (!few || b.lddy < (1 << 24));
-    Operand g{c.g, pad8(N), pad8(N)};
-    if (products && same && !few)
-        if (hipError_t e = operand<T>(c, b.dY, b.lddy, M, N, c.g, &g)) return e;
+    // The products take g rounded to a 16-bit type, a rounding more than their result's own.
+    // Of up to 64 rows, where it would show (an element of g is in every value of a row of
+    // dX) and W or latency is the bound, what it left goes along as a second value.
+    const bool rest = sizeof(T) == 2 && few && M <= 64 && !same;
+    // What goes to linear_skinny.hip: dX of few_rows; dW (us there and on tiles: bf16 256 x
+    // 1,024 x 1,024 7.4 and 14.4, 512 x 512 x 512 10.5 and 9.0, 2,000 x 64 x 64 126 and 9.5; fp32 64
+    // x 4,096 x 4,096 59 and 40, 128 x 1,024 x 1,024 9.4 and 16)
+    const bool outer = few && (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)));
+    Operands o(c);
+    Operand x{}, w{c.W, N, N}, g{c.g, pad8(N), pad8(N)};
+    if (same && products) {
+        if (few && (outer || !b.dW)) g = Operand{b.dY, b.lddy, N};
+        else g = o.get<T>(b.dY, b.lddy, M, N, c.g);
+    }
+    // (16-bit rows that start at odd elements load slowly: where many rows of g read W, it is
+    // laid out first for k_skinny too: 333 x 777 x 1,001 in bf16 19.6 us, 17.9 so; not at 100 x
+    // 255 x 257, 8.5 and 11.6, nor where N is even, 333 x 776 x 1,002 9.7 and 15.6)
+    if (b.dX && M > 0 && (!few || (sizeof(T) == 2 && M > 128 && N % 2))) w = o.get<T>(c.W, N, K, N, c.w);
+    if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x);
+    if (hipError_t e = o.launch<T>()) return e;
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
         GradArgs a;
@@ -271,7 +314,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.Z = b.Z;
         a.dY = b.dY;
         a.G = products && !same ? c.g : nullptr;
-        a.low = sizeof(T) == 2 && few && a.G ? c.low : nullptr;
+        a.low = rest && a.G ? c.low : nullptr;
         a.col = b.db && chunks > 1 ? c.col : nullptr;
         a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
@@ -290,43 +333,21 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         if (hipError_t e = hipGetLastError()) return e;
     }
     Epilogue e{};
-    if (few) {
-        const void *G = same ? b.dY : c.g;
-        const int64_t ldg = same ? b.lddy : pad8(N);
-        // The tiles take g rounded to a 16-bit type, once more than its result; here, where
-        // few terms would show it and W or latency is the bound, the rest goes along.
-        const int64_t low = sizeof(T) == 2 && !same ? (T *)c.low - (T *)c.g : 0;
+    if (b.dX && M > 0) {
         e.Y = b.dX;
         e.ldy = b.lddx;
-        if (b.dX && M > 0)
-            if (hipError_t s = launch_skinny(GEMM_NT, c.dtype, G, ldg, low, c.W, N, M, K, N, e, c.part,
-                                             c.part_floats, c.arrived, c.arrived_words, c.stream))
-                return s;
-        // (dW, us here and on tiles: bf16 256 x 1,024 x 1,024 7.5 and 14.4, 512 x 512 x 512 11.0
-        // and 9.0, 2,000 x 64 x 64 126 and 9.5; fp32 64 x 4,096 x 4,096 59 and 37)
-        if (!b.dW) return hipSuccess;
-        if (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)))
-            return launch_outer(c.dtype, b.X, b.ldx, G, ldg, low, M, K, N, b.dW, c.stream);
-        if (same)
-            if (hipError_t s = operand<T>(c, G, ldg, M, N, c.g, &g)) return s;
+        const hipError_t s =
+            few ? launch_skinny(GEMM_NT, c.dtype, g.p, g.ld, rest ? (T *)c.low - (T *)c.g : 0, w.p, w.ld, M, K, N, e,
+                                c.part, c.part_floats, c.arrived, c.arrived_words, c.stream)
+                : launch_gemm(GEMM_NT, c.dtype, g, w, M, K, N, e, c.part, c.part_floats, c.stream);
+        if (s != hipSuccess) return s;
     }
-    if (b.dX && !few) {
-        Operand w;
-        if (hipError_t s = operand<T>(c, c.W, N, K, N, c.w, &w)) return s;
-        e.Y = b.dX;
-        e.ldy = b.lddx;
-        if (hipError_t s = launch_gemm(GEMM_NT, c.dtype, g, w, M, K, N, e, c.part, c.part_floats, c.stream))
-            return s;
-    }
-    if (b.dW) {
-        Operand x;
-        if (hipError_t s = operand<T>(c, b.X, b.ldx, M, K, c.x, &x)) return s;
-        e.Y = b.dW;
-        e.ldy = N;
-        if (hipError_t s = launch_gemm(GEMM_TN, c.dtype, x, g, K, N, M, e, c.part, c.part_floats, c.stream))
-            return s;
-    }
-    return hipSuccess;
+    if (!b.dW) return hipSuccess;
+    if (outer)
+        return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, rest ? (T *)c.low - (T *)c.g : 0, M, K, N, b.dW, c.stream);
+    e.Y = b.dW;
+    e.ldy = N;
+    return launch_gemm(GEMM_TN, c.dtype, x, g, K, N, M, e, c.part, c.part_floats, c.stream);
 }
 
 __global__ __launch_bounds__(256) void k_clear(uint32_t *p, int64_t n) {
