@@ -188,12 +188,12 @@ static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t 
            d_out <= LINEAR_MAX_WIDTH && max_rows >= 1 && max_rows <= MLP_MAX_BATCH;
 }
 
-// Workspace: the operands g, X and W, the partial column sums, the partial products, the
-// arrival counts.
+// Workspace (ws null: its size alone): the operands g, X and W, the partial column sums, the
+// partial products, the arrival counts.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
-        char *p = ws + at;
+        char *p = ws ? ws + at : nullptr;
         at += pad256(bytes);
         return p;
     };

@@ -106,6 +106,15 @@ def test_in_place(mlp):
     assert grad.shape == want.shape
 
 
+def test_nothing_dropped(mlp):
+    """p = 0 without residual and out: the input itself; with one of them a copy."""
+    x = torch.randn(5, 9, device="cuda")
+    assert mlp.mlp_dropout_forward(x, 0.0, None) is x and mlp.mlp_dropout_backward(x, 0.0, None) is x
+    out = torch.empty_like(x)
+    assert mlp.mlp_dropout_forward(x, 0.0, None, out=out) is out and torch.equal(out, x)
+    assert torch.equal(mlp.mlp_dropout_forward(x, 0.0, None, residual=x), x + x)
+
+
 def test_empty(mlp):
     for shape in ((0, 8), (8, 0), (0, 0)):
         x = torch.empty(*shape, device="cuda")

@@ -290,6 +290,77 @@ def test_own_stream(mlp):  # noqa: F811
     assert torch.equal(mlp.mlp_linear_forward(ctx, x), want[0])
 
 
+def test_calls_follow_one_another_over_streams(mlp):  # noqa: F811
+    """A context without a stream of its own, made on one stream and called on others: a
+    call comes after the ones before it, whose workspace it shares (the split sums and
+    arrival counts of few rows, g of the backward call)."""
+    g = torch.Generator().manual_seed(7)
+    W, b = _layer(g, 4096, 256, "bf16", True)
+    _, x = _rows(g, 6, 4096, "bf16", 0)
+    _, dy = _rows(g, 6, 256, "bf16", 0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    with torch.cuda.stream(streams[0]):
+        ctx = mlp.mlp_linear_init(W, b, "silu", max_rows=6)
+    state, out = _rng(1, 2), []
+    torch.cuda.synchronize()
+    for i in range(12):
+        with torch.cuda.stream(streams[i % 3]):
+            y, z = mlp.mlp_linear_forward(ctx, x, save_z=True)
+            out.append((y, z) + mlp.mlp_linear_backward(ctx, x, dy, z=z, p=0.5, rng=state))
+    torch.cuda.synchronize()
+    ry, rz, by, bz = R.forward(x, W, b, None, "silu", 0.0, None, "bf16")
+    R.check("y", out[0][0], ry, by)
+    R.check("z", out[0][1], rz, bz)
+    for o in out[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(o, out[0]))
+
+
+def test_two_contexts_at_once(mlp):  # noqa: F811
+    """Two layers with workspaces of their own, on two streams at the same time."""
+    g = torch.Generator().manual_seed(8)
+    jobs = []
+    for rows, d_in, d_out in ((5, 4096, 384), (700, 520, 264)):
+        W, b = _layer(g, d_in, d_out, "bf16", True)
+        _, x = _rows(g, rows, d_in, "bf16", 0)
+        s = torch.cuda.Stream()
+        ctx = mlp.mlp_linear_init(W, b, "relu", max_rows=rows, stream=s.cuda_stream)
+        want = R.forward(x, W, b, None, "relu", 0.0, None, "bf16")
+        jobs.append((ctx, x, s, want))
+    torch.cuda.synchronize()
+    got = [[mlp.mlp_linear_forward(ctx, x) for ctx, x, _, _ in jobs] for _ in range(20)]
+    torch.cuda.synchronize()
+    for j, (_, _, _, want) in enumerate(jobs):
+        R.check("y", got[0][j], want[0], want[2])
+        assert all(torch.equal(o[j], got[0][j]) for o in got)
+
+
+def test_few_rows_in_a_graph(mlp):  # noqa: F811
+    """Split sums and their arrival counts over replays, with eager calls in between."""
+    g = torch.Generator().manual_seed(9)
+    W, b = _layer(g, 4096, 384, "bf16", True)
+    _, x = _rows(g, 3, 4096, "bf16", 0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        ctx = mlp.mlp_linear_init(W, b, "gelu_tanh", max_rows=20)
+        y = mlp.mlp_linear_forward(ctx, x)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=s):
+            mlp.mlp_linear_forward(ctx, x, out=y)
+        for k in range(5):
+            gr.replay()
+            gr.replay()
+            torch.cuda.synchronize()
+            replayed = y.clone()
+            assert torch.equal(mlp.mlp_linear_forward(ctx, x), replayed)
+            ry, _, by, _ = R.forward(x, W, b, None, "gelu_tanh", 0.0, None, "bf16")
+            R.check("y", replayed, ry, by)
+            x.mul_(-0.75)
+            torch.cuda.synchronize()
+
+
 def test_refusals(mlp):  # noqa: F811
     W = torch.zeros(16, 24, device="cuda")
     b = torch.zeros(24, device="cuda")
