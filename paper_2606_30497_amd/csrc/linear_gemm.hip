@@ -219,6 +219,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
         int c = 0;
         for (; left >= BK; ++c) chunk(std::false_type());
         for (; c < nk; ++c) chunk(std::true_type());
+        loaded_all_but<0>();   // no load to LDS is under way when the results take its place
     }
 
     finish_tile<T>(g, at, wm, wn, acc, reinterpret_cast<float *>(lds));
