@@ -201,8 +201,9 @@ __device__ __forceinline__ void activate_back8(int act, const float (&z)[8], flo
     case MLP_ACT_GELU_TANH:
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float s = sigmoid(GELU_C * (z[j] + GELU_A * z[j] * z[j] * z[j]));
-            v[j] *= s + z[j] * s * (1.0f - s) * GELU_C * (1.0f + 3.0f * GELU_A * z[j] * z[j]);
+            // (s is 0 or 1 long before z^2 = 10^4; past it z^2 would become infinite)
+            const float zz = GELU_A * fminf(z[j] * z[j], 1e4f), s = sigmoid(GELU_C * fmaf(z[j], zz, z[j]));
+            v[j] *= s + z[j] * s * (1.0f - s) * GELU_C * fmaf(3.0f, zz, 1.0f);
         }
         break;
     case MLP_ACT_SILU:

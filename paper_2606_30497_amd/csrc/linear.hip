@@ -427,8 +427,8 @@ extern "C" mlp_status mlp_linear_forward(mlp_linear_t c, const void *X, int64_t 
     Epilogue e{};
     if (!c || rows < 0 || rows > c->max_rows || !make_drop(p, rng, &e.drop)) return MLP_ERR_INVALID_ARG;
     if (rows == 0) return MLP_OK;
-    if (!X || !Y || X == Y || Z == Y || Z == X || Y == c->W || Z == c->W || (Z && Z == residual) ||
-        (residual == Y && ldr != ldy))
+    if (!X || !Y || X == Y || Z == Y || Z == X || Y == c->W || Z == c->W || Y == c->bias ||
+        (Z && (Z == residual || Z == c->bias)) || (residual == Y && ldr != ldy))
         return MLP_ERR_INVALID_ARG;
     if (!stride_ok(ldx, rows, c->d_in) || !stride_ok(ldy, rows, c->d_out) ||
         (residual && !stride_ok(ldr, rows, c->d_out)) || (Z && !stride_ok(ldz, rows, c->d_out)))
@@ -452,11 +452,11 @@ extern "C" mlp_status mlp_linear_backward(mlp_linear_t c, const void *X, int64_t
                                           void *dbias) {
     BackwardArgs b;
     if (!c || rows < 0 || rows > c->max_rows || !make_drop(p, rng, &b.drop)) return MLP_ERR_INVALID_ARG;
+    for (const void *o : {(const void *)dX, (const void *)dW, (const void *)dbias})
+        if (o && (o == X || o == Z || o == dY || o == c->W || o == c->bias)) return MLP_ERR_INVALID_ARG;
+    if ((dX && (dX == dW || dX == dbias)) || (dW && dW == dbias)) return MLP_ERR_INVALID_ARG;
     if (rows > 0) {
         if (!dY || (dW && !X) || (c->act != MLP_ACT_NONE && !Z)) return MLP_ERR_INVALID_ARG;
-        for (const void *o : {(const void *)dX, (const void *)dW, (const void *)dbias})
-            if (o && (o == X || o == Z || o == dY || o == c->W || o == c->bias)) return MLP_ERR_INVALID_ARG;
-        if ((dX && (dX == dW || dX == dbias)) || (dW && dW == dbias)) return MLP_ERR_INVALID_ARG;
         if (!stride_ok(lddy, rows, c->d_out) || (dW && !stride_ok(ldx, rows, c->d_in)) ||
             (c->act != MLP_ACT_NONE && !stride_ok(ldz, rows, c->d_out)) ||
             (dX && !stride_ok(lddx, rows, c->d_in)))

@@ -651,13 +651,13 @@ def _dropout_call(fn, X, p, rng, residual, out, name):
         raise TypeError("%s must be one of %s" % (name, tuple(DTYPES)))
     if not X.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    p = float(p)
+    if p == 0.0 and out is None and residual is None:
+        return X
     rows, cols = X.shape
     xp, ldx = _mat(X, name, dt, dev, rows, cols)
     rp, ldr = _mat(residual, "residual", dt, dev, rows, cols)
     gp = _rng(rng, dev)
-    p = float(p)
-    if p == 0.0 and out is None and residual is None:
-        return X
     if out is None:
         out = torch.empty((rows, cols), dtype=dt, device=dev)
         yp, ldy = out.data_ptr(), cols

@@ -402,3 +402,34 @@ def test_refusals(mlp):  # noqa: F811
         mlp.mlp_linear_init(W.double(), None, "relu", max_rows=8)
     torch.cuda.synchronize()
     assert bool((y == 5.0).all())
+
+
+@pytest.mark.parametrize("act", R.ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_activations_far_out(mlp, dtype, act):  # noqa: F811
+    """a(z) and a'(z) where powers of z leave fp32: of one row through the unit matrix."""
+    big = [0.0, 3.0, 20.0, 100.0, 1e4, 6e4] + ([] if dtype == "f16" else [1e19, 1e20, 3e38])
+    z = torch.tensor([[s * v for v in big for s in (1, -1)]]).to(R.DTYPES[dtype]).cuda()
+    n = z.shape[1]
+    ctx = mlp.mlp_linear_init(torch.eye(n, device="cuda", dtype=z.dtype), torch.zeros_like(z[0]), act, max_rows=1)
+    y = mlp.mlp_linear_forward(ctx, z)
+    _, _, db = mlp.mlp_linear_backward(ctx, None, torch.ones_like(z), z=z, need_dx=False, need_dw=False)
+    u, zd = R.U[dtype], z.cpu().double()
+    # the functions to a few 2^-24 of their terms, |z| of them no more than where they have
+    # not reached their ends (20), and the rounding of the result
+    for got, want, size in ((y, R.act(zd, act), zd.abs()), (db[None], R.act_grad(zd, act), zd.abs().clamp(max=20))):
+        R.check(act, got, want, u * want.abs() + 16 * R.E * (1 + size) + R.TINY[dtype])
+
+
+@pytest.mark.parametrize("rows", [0, 4])
+def test_outputs_that_are_parameters(mlp, rows):  # noqa: F811
+    """No call takes W or the bias as an output, not of no rows either."""
+    W = torch.ones(16, 16, device="cuda")
+    b = torch.ones(16, device="cuda")
+    ctx = mlp.mlp_linear_init(W, b, max_rows=4)
+    x = torch.ones(rows, 16, device="cuda")
+    for bad in (dict(dW=W), dict(db=b)):
+        with pytest.raises(mlp.MLPError):
+            mlp.mlp_linear_backward(ctx, x, torch.ones_like(x), **bad)
+    torch.cuda.synchronize()
+    assert bool((W == 1).all()) and bool((b == 1).all())
