@@ -4,7 +4,8 @@
 // Every element is read and written once: the call is bound by memory (bf16: 4 bytes an
 // element, 6 with a residual). A thread takes eight consecutive columns of a row, one
 // block of the generator (20 products of 32 x 32 bits, a quarter of the vector rate):
-// with 16 bits an element its instructions take about half the time of the traffic.
+// with 16 bits an element its instructions take about half the time of the traffic. bf16
+// 16,384 x 8,192 in 148 us, 5.4 TB/s (a 4 GiB copy: 4.75); 7 x 1,000, a launch: 2 us.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>

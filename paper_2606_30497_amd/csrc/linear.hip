@@ -66,7 +66,9 @@ __global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
 }
 
 // g = dropout(dY) a'(z) and its partial column sums: a workgroup takes a chunk of rows
-// and 8 * groups columns.
+// and 8 * groups columns, a thread eight columns of every 256 / groups rows, the next row's
+// on their way. Bound by memory and the derivative's arithmetic (8,192 x 4,096 in bf16,
+// GELU: 65 us, 3.1 TB/s).
 struct GradArgs {
     const void *Z, *dY;
     void *G;                  // nullable, an operand of rows of pad8(N)
@@ -242,20 +244,24 @@ struct Operands {
     }
 };
 
-// Whether the products of M rows go to linear_skinny.hip: those of a few rows, and small
-// ones (us here and on tiles, bf16: 512 x 512 x 512 7.0 and 9.1, 256 x 1,024 x 1,024 7.9 and
-// 11.6, 333 x 776 x 1,000 8.5 and 10.6, 8,192 x 256 x 256 9.2 and 7.7; fp32, whose tiles'
-// operands are packed first: 128 x 1,024 x 1,024 10 and 21, 64 x 4,096 x 4,096 34 and 65,
-// 512 x 1,024 x 1,024 27 and 32).
-static bool few_rows(const LinearCtx &c, int64_t M) {
+// Whether the products of M rows with W go to linear_skinny.hip: those of a few rows, and
+// small ones, the deep ones among them up to a larger size, since on tiles their depth is
+// split over many (us here and on tiles; y in bf16: 1,024 x 512 x 512 5.8 and 6.4, with 2^29
+// products, 2,048 x 512 x 512, 6.8 and 6.7; in fp32: 128 x 1,024 x 1,024 10 and 13, 512 x 1,024 x
+// 1,024 21 and 19, 100 x 16,384 x 300 30 and 52; dX in fp32: 512 x 512 x 512 11 and 13, 256 x
+// 1,024 x 1,024 16 and 15, 100 x 300 x 16,384 32 and 37; in bf16: 64 x 1,024 x 1,024 8.4 and 8.4,
+// 256 x 1,024 x 1,024 10.2 and 8.5, 100 x 30 x 10,001 14 and 28).
+static bool few_rows(const LinearCtx &c, int64_t M, bool back) {
     if (c.d_in < SKINNY_WIDTH || c.d_out < SKINNY_WIDTH) return false;
-    const int64_t small = c.dtype == MLP_F32 ? 1 << 29 : 1 << 28;
-    return M <= (c.dtype == MLP_F32 ? 64 : 32) || (M <= FEW_ROWS && M * c.d_in * c.d_out <= small);
+    const bool f32 = c.dtype == MLP_F32, deep = (back ? c.d_out : c.d_in) > 4096;
+    const int64_t rows = back && !f32 && !deep ? 64 : FEW_ROWS;
+    const int64_t size = !f32 ? 1 << 28 : deep ? 1 << 29 : back ? 1 << 27 : 1 << 28;
+    return M <= (f32 ? 64 : 32) || (M <= rows && M * c.d_in * c.d_out <= size);
 }
 
 template <class T>
 static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx, int64_t rows, const Epilogue &e) {
-    if (few_rows(c, rows))
+    if (few_rows(c, rows, false))
         return launch_skinny(GEMM_NN, c.dtype, X, ldx, 0, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
                              c.part_floats, c.arrived, c.arrived_words, c.stream);
     Operands o(c);
@@ -275,7 +281,7 @@ struct BackwardArgs {
 template <class T>
 static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     const int64_t M = b.rows, N = c.d_out, K = c.d_in;
-    const bool products = M > 0 && (b.dX || b.dW), few = few_rows(c, M);
+    const bool products = M > 0 && (b.dX || b.dW), few = few_rows(c, M, true);
     // without activation and dropout g is dY, and dY itself the operand (of few rows, where
     // 32-bit offsets reach over the depth of a step)
     const bool same = c.act == MLP_ACT_NONE && !b.drop.rng && (!few || b.lddy < (1 << 24));
@@ -283,10 +289,9 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // Of up to 64 rows, where it would show (an element of g is in every value of a row of
     // dX) and W or latency is the bound, what it left goes along as a second value.
     const bool rest = sizeof(T) == 2 && few && M <= 64 && !same;
-    // What goes to linear_skinny.hip: dX of few_rows; dW (us there and on tiles: bf16 256 x
-    // 1,024 x 1,024 7.4 and 14.4, 512 x 512 x 512 10.5 and 9.0, 2,000 x 64 x 64 126 and 9.5; fp32 64
-    // x 4,096 x 4,096 59 and 40, 128 x 1,024 x 1,024 9.4 and 16)
-    const bool outer = few && (M <= 32 || (M <= 256 && M * K * N <= (sizeof(T) == 4 ? 1 << 27 : 1 << 28)));
+    // what goes to linear_skinny.hip: dX of few_rows, and dW of 32 rows (us there and on
+    // tiles, 4,096 x 4,096: bf16 12.5 and 14.6, fp32 33 and 33) or, for the second values, 64
+    const bool outer = few && M <= (sizeof(T) == 4 ? 32 : 64);
     Operands o(c);
     Operand x{}, w{c.W, N, N}, g{c.g, pad8(N), pad8(N)};
     if (same && products) {
@@ -294,8 +299,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         else g = o.get<T>(b.dY, b.lddy, M, N, c.g);
     }
     // (16-bit rows that start at odd elements load slowly: where many rows of g read W, it is
-    // laid out first for k_skinny too: 333 x 777 x 1,001 in bf16 19.6 us, 17.9 so; not at 100 x
-    // 255 x 257, 8.5 and 11.6, nor where N is even, 333 x 776 x 1,002 9.7 and 15.6)
+    // laid out first for k_skinny too: 700 x 30 x 10,001 in bf16 29 us, 20 so)
     if (b.dX && M > 0 && (!few || (sizeof(T) == 2 && M > 128 && N % 2))) w = o.get<T>(c.W, N, K, N, c.w);
     if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x);
     if (hipError_t e = o.launch<T>()) return e;

@@ -237,13 +237,23 @@ __global__ __launch_bounds__(256) void k_gemm_join(const GemmArgs g) {
         if (g.e.R) res = fetch8((const T *)g.e.R + m * g.e.ldr, n, g.N);
         float v[8];
         load8(g.part + m * g.N, n, g.N, v);
-#pragma unroll 4
-        for (int s = 1; s < g.splits; ++s) {
-            float w[8];
-            load8(g.part + (s * g.M + m) * g.N, n, g.N, w);
+        auto add = [&](const Oct<float> &w) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += w[j];
+            for (int j = 0; j < 8; ++j) v[j] += w.e[j];
+        };
+        const float *p = g.part + m * g.N;
+        int s = 1;
+        // sixteen loads under way at a time: few outputs have many splits (dW of 65,536 x 64 x
+        // 64 in bf16 35 us in all, 40 with four)
+        for (; s + 16 <= g.splits; s += 16) {
+            Oct<float> w[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) w[q] = fetch8(p + (s + q) * g.M * g.N, n, g.N);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) add(w[q]);
         }
+#pragma unroll 4
+        for (; s < g.splits; ++s) add(fetch8(p + s * g.M * g.N, n, g.N));
         fin.finish(g.e, m, n, g.N, v, res);
     }
 }
@@ -259,23 +269,34 @@ template hipError_t join_splits<float>(const GemmArgs &, hipStream_t);
 
 template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN>
 static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream) {
-    const unsigned grid = plan_tiles(g, TM, TN, BK, part_floats);
+    // (a chunk of 64 takes 0.28 us on 64 x 64 tiles, 0.5 on 128 x 128, 1 and more on 256 x 256)
+    constexpr int WORTH = (TM == 64 ? 1024 : TM == 128 ? 576 : 256) / BK;
+    const unsigned grid = plan_tiles(g, TM, TN, BK, CUS, WORTH, part_floats);
     hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, S, WM, WN>), dim3(grid), dim3(64 * WM * WN), 0, stream, g);
     if (hipError_t e = hipGetLastError()) return e;
     return join_splits<T>(g, stream);
 }
 
-// Tiles by their number (us, bf16, NN and NT: 2,048 x 4,096 x 4,096 70 on the 128 x 128 tiles
-// of two stages, which run two workgroups a compute unit, 81 on those of four; 1,776 x 1,000 x
-// 2,048 14 on four stages and eight waves, 20 on two and four).
+// The tile by the number of tiles (us in bf16, of outputs x depth):
+// 256 x 256 where there are more than half as many as compute units, which run one each, and
+// they cover at most 5/4 of what 128 x 128 would (3,328 x 3,328 x 1,024 33, on 128 x 128 38; 2,816 x
+// 2,816 x 1,024, split in two, 49 and 24; 131,072 x 128 x 256 37 and 25);
+// 128 x 128 of two stages, two workgroups a compute unit, where there are more than units
+// (2,304 x 2,304 x 2,048 34, of four stages 40; 2,048 x 2,048 x 2,048 34 and 24; TN's stages
+// are half as deep, and two workgroups run with four of them);
+// 128 x 128 of four stages where no split is needed (1,536 x 1,536 x 1,536 18, on 64 x 64 22),
+// or the depth pays for the splits' joining (1,024 x 1,024 x 16,384 58 and 76, of 1,024 23 and
+// 8.6; TN, whose 64 x 64 tiles are slower, of 4,096 27 and 36, of 2,048 22 and 14).
 template <class T, int OP>
 static hipError_t gemm_op(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
     constexpr bool TN = OP == GEMM_TN;
     const int64_t big = ceil_div(g.M, 256) * ceil_div(g.N, 256), mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
-    if (big >= 200) return gemm_tiles<T, OP, 256, 256, TN ? 32 : 64, TN ? 5 : 2, 2, 4>(g, part_floats, stream);
+    if (big > CUS / 2 && 16 * big <= 5 * mid)
+        return gemm_tiles<T, OP, 256, 256, TN ? 32 : 64, TN ? 5 : 2, 2, 4>(g, part_floats, stream);
     if constexpr (!TN)
-        if (mid >= 400) return gemm_tiles<T, OP, 128, 128, 64, 2, 2, 2>(g, part_floats, stream);
-    if (mid >= 32) return gemm_tiles<T, OP, 128, 128, TN ? 32 : 64, 4, 2, TN ? 2 : 4>(g, part_floats, stream);
+        if (mid > CUS) return gemm_tiles<T, OP, 128, 128, 64, 2, 2, 2>(g, part_floats, stream);
+    if (mid > CUS / 2 || (mid >= 16 && g.K > (TN ? 2048 : 4096)))
+        return gemm_tiles<T, OP, 128, 128, TN ? 32 : 64, 4, 2, TN ? 2 : 4>(g, part_floats, stream);
     return gemm_tiles<T, OP, 64, 64, 64, 4, 2, 2>(g, part_floats, stream);
 }
 

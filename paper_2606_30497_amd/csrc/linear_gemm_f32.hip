@@ -221,19 +221,31 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_f32(const GemmArgs g) {
 
 template <int OP, int TM, int TN, int WM, int WN>
 static hipError_t tiles_f32(GemmArgs g, int64_t part_floats, hipStream_t stream) {
-    const unsigned grid = plan_tiles(g, TM, TN, FK, part_floats);
+    // (A chunk takes 0.5 us on 64 x 64 tiles, 1.3 on 128 x 128. Where many 64 x 64 tiles are
+    // deep, two workgroups a compute unit: 700 x 16,384 x 300 196 us with one, 103 with two;
+    // dW of 3,000 x 10,001 x 30 141 and 64; 1,024 x 1,024 x 1,024 22 and 27)
+    const bool two = TM == 64 && g.K > 64 * FK && ceil_div(g.M, TM) * ceil_div(g.N, TN) >= 32;
+    const unsigned grid = plan_tiles(g, TM, TN, FK, two ? 2 * CUS : CUS, TM == 64 ? 9 : 4, part_floats);
     hipLaunchKernelGGL((k_gemm_f32<OP, TM, TN, WM, WN>), dim3(grid), dim3(64 * WM * WN), 0, stream, g);
     if (hipError_t e = hipGetLastError()) return e;
     return join_splits<float>(g, stream);
 }
 
+// The tile by the number of tiles, 64 x 64 where larger ones would cover over 5/4 of what
+// those do (65,536 x 64 x 1,024 on 64 x 64 84 us, on 128 x 128 144, 65,536 x 192 x 256 56 and
+// 71):
+// 256 x 128 where there are many (us, of outputs x depth: 4,096 x 2,048 x 2,048 191, on 128 x
+// 128 205; 2,048 x 2,048 x 2,048 106 and 94; TN, which spills 29 registers, 4,096 x 4,096 x
+// 8,192 1,586 and 1,645, 4,096 x 2,048 x 2,048 244 and 209);
+// 128 x 128 where no split is needed (2,048 x 2,048 x 2,048 94, on 64 x 64 125) or the depth pays
+// for the splits' joining (1,024 x 1,024 x 2,048 40 and 52, of 1,024 29 and 23).
 template <int OP>
 static hipError_t op_f32(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
     const int64_t mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
-    // (TN at 256 x 128 spills 29 registers, and is the faster all the same: 8,192 x 4,096 x
-    // 4,096 1,586 us, 1,645 at 128 x 128)
-    if (mid >= 400) return tiles_f32<OP, 256, 128, 4, 2>(g, part_floats, stream);
-    if (mid >= 32) return tiles_f32<OP, 128, 128, 2, 4>(g, part_floats, stream);
+    if (16 * mid <= 5 * ceil_div(g.M, 64) * ceil_div(g.N, 64)) {
+        if (mid >= (OP == GEMM_TN ? 1024 : 400)) return tiles_f32<OP, 256, 128, 4, 2>(g, part_floats, stream);
+        if (mid > CUS / 2 || (mid >= 16 && g.K > 1024)) return tiles_f32<OP, 128, 128, 2, 4>(g, part_floats, stream);
+    }
     return tiles_f32<OP, 64, 64, 2, 2>(g, part_floats, stream);
 }
 

@@ -148,17 +148,20 @@ __device__ __forceinline__ void finish_tile(const GemmArgs &g, const TileAt &at,
     }
 }
 
+constexpr int CUS = 256;
+
 // The launch plan of TM x TN tiles and chunks of BK: splits of the depth where the tiles
-// are fewer than the compute units, of four chunks at least, as far as there is room.
-inline unsigned plan_tiles(GemmArgs &g, int TM, int TN, int BK, int64_t part_floats) {
-    constexpr int64_t CUS = 256;
+// are fewer than `most` workgroups, of four chunks at least, as far as there is room, and
+// where they spare a tile at least `worth` chunks, the time of the splits' joining (a launch
+// and the sums' way through memory: 4 to 5 us).
+inline unsigned plan_tiles(GemmArgs &g, int TM, int TN, int BK, int most, int worth, int64_t part_floats) {
     g.tiles_m = (int)ceil_div(g.M, TM);
     g.tiles_n = (int)ceil_div(g.N, TN);
     const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n, chunks = ceil_div(g.K, BK);
-    int64_t splits = tiles < CUS ? CUS / tiles : 1;
+    int64_t splits = tiles < most ? most / tiles : 1;
     if (splits > chunks / 4) splits = chunks / 4;
     if (splits > part_floats / (g.M * g.N)) splits = part_floats / (g.M * g.N);
-    if (splits < 1) splits = 1;
+    if (splits < 1 || chunks - ceil_div(chunks, splits) < worth) splits = 1;
     g.kc = ceil_div(chunks, splits) * BK;
     g.splits = g.K > 0 ? (int)ceil_div(g.K, g.kc) : 1;
     return (unsigned)(tiles * g.splits);
