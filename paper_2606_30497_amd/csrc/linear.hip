@@ -259,11 +259,24 @@ static bool few_rows(const LinearCtx &c, int64_t M, bool back) {
     return M <= (f32 ? 64 : 32) || (M <= rows && M * c.d_in * c.d_out <= size);
 }
 
+// Whether y of fewer than eight outputs goes to k_narrow (us there and on tiles, rows x depth x
+// outputs; fp32: 64 x 256 x 7 6.0 and 11, 3,000 x 256 x 7 10.4 and 11, 65,536 x 256 x 1 32 and
+// 33, 65,536 x 1,024 x 3 56 and 107, 65,536 x 1,024 x 7 154 and 105, 3,000 x 16,384 x 3 38 and 93; bf16,
+// whose values take an instruction more each and half of the bytes: 64 x 1,024 x 7 7.4 and
+// 10.5, 64 x 256 x 7 7.6 and 7.0, 3,000 x 4,097 x 7 29 and 31, 65,536 x 1,024 x 1 68 and 29).
+static bool narrow(const LinearCtx &c, int64_t M) {
+    if (c.d_out >= SKINNY_WIDTH) return false;
+    if (c.dtype != MLP_F32) return M <= 2048 && c.d_in >= 128 * c.d_out;
+    return c.d_in >= (M <= 1024 ? 128 : 256 * c.d_out);
+}
+
 template <class T>
 static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx, int64_t rows, const Epilogue &e) {
     if (few_rows(c, rows, false))
         return launch_skinny(GEMM_NN, c.dtype, X, ldx, 0, c.W, c.d_out, rows, c.d_out, c.d_in, e, c.part,
                              c.part_floats, c.arrived, c.arrived_words, c.stream);
+    if (narrow(c, rows))
+        return launch_narrow(c.dtype, X, ldx, c.W, rows, c.d_out, c.d_in, e, c.stream);
     Operands o(c);
     const Operand x = o.get<T>(X, ldx, rows, c.d_in, c.x), w = o.get<T>(c.W, c.d_out, c.d_in, c.d_out, c.w);
     if (hipError_t s = o.launch<T>()) return s;

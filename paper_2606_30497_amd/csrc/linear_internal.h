@@ -93,6 +93,9 @@ constexpr int64_t SKINNY_WIDTH = 8;
 hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, int64_t low, const void *W,
                          int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue &e, float *part,
                          int64_t part_floats, uint32_t *arrived, int64_t arrived_words, hipStream_t stream);
+// Y = X W of N < SKINNY_WIDTH outputs
+hipError_t launch_narrow(int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t M, int64_t N, int64_t K,
+                         const Epilogue &e, hipStream_t stream);
 // dW [K x N] = X^T G of M rows, N >= SKINNY_WIDTH; low as above, of G
 hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t low,
                         int64_t M, int64_t K, int64_t N, void *dW, hipStream_t stream);

@@ -14,6 +14,9 @@
 //
 // k_outer, dW = X^T g of few rows: the same products with X read across its rows; a wave
 // takes 16 x 128 values of dW, bound by writing them.
+//
+// k_narrow, y = x W of fewer than eight outputs and a deep row: no matrix instruction, whose
+// columns would be idle; bound by reading X.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -452,6 +455,94 @@ hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G
     }
 #undef OUTER
     return hipGetLastError();
+}
+
+// N outputs of eight rows: a workgroup's lanes share the depth, eight k a lane and step (W's
+// 8 N values of those are contiguous), fp32 sums joined over the lanes and, in LDS, the waves.
+template <class T, int N>
+__global__ __launch_bounds__(512) void k_narrow(const T *X, int64_t ldx, const T *W, int64_t M, int64_t K, const Epilogue e) {
+    constexpr int R = 8, WAVES = 8;
+    __shared__ float sums[WAVES][R][N];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t m0 = (int64_t)blockIdx.x * R;
+    float acc[R][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[r][j] = 0.0f;
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * 512) {
+        Oct<T> x[R], w[N];
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = fetch8(X + (m0 + r < M ? m0 + r : M - 1) * ldx, k, K);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = fetch8(W, k * N + 8 * i, K * N);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float f = up(w[(i * N + j) / 8].e[(i * N + j) % 8]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) acc[r][j] = fmaf(up(x[r].e[i]), f, acc[r][j]);
+            }
+    }
+    // over the lanes: half of them take half of the rows, and so on (10 N exchanges)
+#pragma unroll
+    for (int h = 4, s = 32; h > 0; h >>= 1, s >>= 1)
+#pragma unroll
+        for (int r = 0; r < h; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float lo = acc[r][j], hi = acc[r + h][j];
+                acc[r][j] = (lane & s ? hi : lo) + __shfl_xor(lane & s ? lo : hi, s);
+            }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+#pragma unroll
+        for (int s = 4; s > 0; s >>= 1) acc[0][j] += __shfl_xor(acc[0][j], s);
+        if ((lane & 7) == 0) sums[wave][(lane >> 3 & 1) + 2 * (lane >> 4 & 1) + 4 * (lane >> 5)][j] = acc[0][j];
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= R || m0 + r >= M) return;
+    float v[8] = {};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v[j] += sums[w][r][j];
+    Finish<T> fin;
+    fin.init(e, 0, N);
+    Oct<T> res;
+    if (e.R) res = fetch8((const T *)e.R + (m0 + r) * e.ldr, 0, N);
+    fin.finish(e, m0 + r, 0, N, v, res);
+}
+
+template <class T>
+static hipError_t narrow_type(const void *X, int64_t ldx, const void *W, int64_t M, int64_t N, int64_t K,
+                              const Epilogue &e, hipStream_t stream) {
+    const dim3 grid((unsigned)ceil_div(M, 8));
+#define NARROW(n) \
+    case n: hipLaunchKernelGGL((k_narrow<T, n>), grid, dim3(512), 0, stream, (const T *)X, ldx, (const T *)W, M, K, e); break
+    switch (N) {
+        NARROW(1);
+        NARROW(2);
+        NARROW(3);
+        NARROW(4);
+        NARROW(5);
+        NARROW(6);
+        NARROW(7);
+    default: return hipErrorInvalidValue;
+    }
+#undef NARROW
+    return hipGetLastError();
+}
+
+hipError_t launch_narrow(int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t M, int64_t N, int64_t K,
+                         const Epilogue &e, hipStream_t stream) {
+    switch (dtype) {
+    case MLP_F32: return narrow_type<float>(X, ldx, W, M, N, K, e, stream);
+    case MLP_BF16: return narrow_type<bf16>(X, ldx, W, M, N, K, e, stream);
+    default: return narrow_type<f16>(X, ldx, W, M, N, K, e, stream);
+    }
 }
 
 }  // namespace mlp

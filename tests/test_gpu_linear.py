@@ -433,3 +433,25 @@ def test_outputs_that_are_parameters(mlp, rows):  # noqa: F811
             mlp.mlp_linear_backward(ctx, x, torch.ones_like(x), **bad)
     torch.cuda.synchronize()
     assert bool((W == 1).all()) and bool((b == 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("d_out", range(1, 8))
+def test_narrow_and_deep(mlp, dtype, d_out):  # noqa: F811
+    """Fewer than eight outputs of a deep row: every width, rows and depths around a step."""
+    for i, (rows, d_in) in enumerate([(1, 511), (3, 512), (9, 1024), (8, 4096), (17, 4099), (33, 8191), (1101, 2050)]):
+        act, p, bias, residual, _ = OPTIONS[(i + d_out) % 5]
+        print(dtype, rows, d_in, d_out, act, p, bias, residual, flush=True)
+        g = torch.Generator().manual_seed(i)
+        W, b = _layer(g, d_in, d_out, dtype, bias)
+        _, x = _rows(g, rows, d_in, dtype, i, float("nan"))
+        r = _rows(g, rows, d_out, dtype, i, float("nan"))[1] if residual else None
+        ybuf, y = _rows(g, rows, d_out, dtype, 2)
+        zbuf, z = _rows(g, rows, d_out, dtype, 1)
+        ctx = mlp.mlp_linear_init(W, b, act, max_rows=rows)
+        mlp.mlp_linear_forward(ctx, x, residual=r, p=p, rng=_rng(5, i), out=y, z=z)
+        torch.cuda.synchronize()
+        ry, rz, by, bz = R.forward(x, W, b, r, act, p, (5, i), dtype)
+        R.check("y", y, ry, by)
+        R.check("z", z, rz, bz)
+        assert bool((ybuf[:, d_out:] == 7.0).all()) and bool((zbuf[:, d_out:] == 7.0).all())
