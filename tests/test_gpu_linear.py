@@ -455,3 +455,29 @@ def test_narrow_and_deep(mlp, dtype, d_out):  # noqa: F811
         R.check("y", y, ry, by)
         R.check("z", z, rz, bz)
         assert bool((ybuf[:, d_out:] == 7.0).all()) and bool((zbuf[:, d_out:] == 7.0).all())
+
+
+# either side of the rules between few rows and tiles, of splits and of deep thin products
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,d_in,d_out", [(300, 40, 5001), (100, 200, 6000), (200, 5000, 24), (600, 4104, 129),
+                                             (520, 776, 520), (48, 4099, 520), (2050, 72, 200), (4100, 260, 136)])
+def test_between_the_rules(mlp, dtype, rows, d_in, d_out):  # noqa: F811
+    print(dtype, rows, d_in, d_out, flush=True)
+    g = torch.Generator().manual_seed(rows)
+    W, b = _layer(g, d_in, d_out, dtype, True)
+    _, x = _rows(g, rows, d_in, dtype, 0)
+    _, dy = _rows(g, rows, d_out, dtype, 1)
+    ctx = mlp.mlp_linear_init(W, b, "silu", max_rows=rows)
+    y, z = mlp.mlp_linear_forward(ctx, x, p=0.1, rng=_rng(3, 4), save_z=True)
+    dx, dw, db = mlp.mlp_linear_backward(ctx, x, dy, z=z, p=0.1, rng=_rng(3, 4))
+    plain = mlp.mlp_linear_init(W, None, "none", max_rows=rows)
+    px, pw, _ = mlp.mlp_linear_backward(plain, x, dy)
+    torch.cuda.synchronize()
+    ry, rz, by, bz = R.forward(x, W, b, None, "silu", 0.1, (3, 4), dtype)
+    R.check("y", y, ry, by)
+    R.check("z", z, rz, bz)
+    for got, (ref, bound) in (((dx, dw, db), R.backward(x, W, z, dy, "silu", 0.1, (3, 4), dtype)),
+                              ((px, pw, None), R.backward(x, W, None, dy, "none", 0.0, None, dtype))):
+        for name, t in zip(("dx", "dw", "db"), got):
+            if t is not None:
+                R.check(name, t, ref[name], bound[name])
