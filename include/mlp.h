@@ -402,8 +402,8 @@ mlp_status mlp_linear_forward(mlp_linear_t ctx, const void *X, int64_t ldx, int6
 /* Gradients for dY = the loss's gradient in Y (which is also the residual's):
  *   g = dropout(dY) a'(Z);  dX = g W^T;  dW = X^T g;  dbias = column sums of g.
  * g is rounded to the call's type for the two products where that is bf16 or fp16 (the
- * matrix cores take such operands), but not for 32 rows or fewer, nor for 64 where the
- * products are not large; dbias is summed from the unrounded g.
+ * matrix cores take such operands), but, widths of 8 and more, not for 32 rows or fewer,
+ * nor for up to 64 where the products are not large; dbias is summed from the unrounded g.
  *   X      [rows x d_in] as in the forward call (used by dW only; may be NULL without)
  *   Z      [rows x d_out] from the forward call; NULL only if the activation is NONE
  *   dY     [rows x d_out];  p, rng as in the forward call

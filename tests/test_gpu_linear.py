@@ -83,7 +83,7 @@ def test_backward(mlp, dtype, rows, d_in, d_out, pad):  # noqa: F811
                 assert got is None or torch.equal(got, want), name
 
 
-# shapes of the larger tiles (200 of 256 x 256, 400 of 128 x 128), a depth that ends inside
+# shapes of the larger tiles (above 128 of 256 x 256, above 256 of 128 x 128), a depth that ends inside
 # a chunk, row tails; whole activations on the CPU would take minutes, so the 64-bit
 # reference is taken of a sample of rows and of columns
 @pytest.mark.parametrize("dtype,rows,d_in,d_out", [("bf16", 3900, 136, 3600), ("f16", 3600, 3336, 300),
