@@ -401,9 +401,11 @@ mlp_status mlp_linear_forward(mlp_linear_t ctx, const void *X, int64_t ldx, int6
 
 /* Gradients for dY = the loss's gradient in Y (which is also the residual's):
  *   g = dropout(dY) a'(Z);  dX = g W^T;  dW = X^T g;  dbias = column sums of g.
- * g is rounded to the call's type for the two products where that is bf16 or fp16 (the
- * matrix cores take such operands), but, widths of 8 and more, not for 32 rows or fewer,
- * nor for up to 64 where the products are not large; dbias is summed from the unrounded g.
+ * For the two products g is rounded to the call's type where that is bf16 or fp16 (the
+ * matrix cores take such operands): the error of dX and dW is then about sqrt(2) times that
+ * of their own rounding. Not so for 32 rows or fewer, nor for up to 64 while rows d_in d_out
+ * <= 2^28 or a width is below 8 (g comes as two values, down to the type's smallest step).
+ * dbias is summed from the unrounded g.
  *   X      [rows x d_in] as in the forward call (used by dW only; may be NULL without)
  *   Z      [rows x d_out] from the forward call; NULL only if the activation is NONE
  *   dY     [rows x d_out];  p, rng as in the forward call

@@ -15,6 +15,7 @@ constexpr int64_t LINEAR_MAX_WIDTH = 1 << 20;
 constexpr int COL_CHUNKS = 256;                   // most row chunks of the column sums
 constexpr int64_t ARRIVED_WORDS = 16384;
 constexpr int64_t FEW_ROWS = 2048;                // most rows of a small product (few_rows)
+constexpr int64_t REST_ROWS = 64;                 // most rows whose g comes in two 16-bit values (linear_backward)
 constexpr int64_t PART_FLOATS_MAX = 256 * 65536;  // 256 workgroups' tiles of partial sums
 
 struct LinearCtx {
@@ -24,7 +25,6 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     void *g = nullptr, *x = nullptr, *w = nullptr;
-    void *low = nullptr;        // what g's rounding to a 16-bit type left (up to 64 rows)
     float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
@@ -37,12 +37,14 @@ struct LinearCtx {
 static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 
 // Matrices of rows x cols to be laid out as operands: rows of pad8(cols) elements, what pads
-// them zero. Read and written once, bound by memory; one launch for all of a call's.
+// them zero; each row 2^twice times. Read and written once, bound by memory; one launch for
+// all of a call's.
 struct PackArgs {
     struct Job {
         const void *P;
         void *out;
-        int64_t ld, rows, cols;
+        int64_t ld, rows, cols;   // rows: of the output
+        int twice;
     } job[3];
     int64_t groups[3];   // of workgroups, up to and with each job's
     int jobs;
@@ -56,11 +58,12 @@ __global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
     const T *P = (const T *)a.job[j].P;
     T *out = (T *)a.job[j].out;
     const int64_t ld = a.job[j].ld, cols = a.job[j].cols;
+    const int twice = a.job[j].twice;
     const int64_t blocks = (cols + 7) / 8, total = a.job[j].rows * blocks;
     for (int64_t i = ((int64_t)blockIdx.x - first) * 256 + threadIdx.x; i < total; i += step) {
         const int64_t r = i / blocks, c = (i - r * blocks) * 8;
         float v[8];
-        load8(P + r * ld, c, cols, v);
+        load8(P + (r >> twice) * ld, c, cols, v);
         store8(out + r * blocks * 8, c, blocks * 8, v);
     }
 }
@@ -71,8 +74,8 @@ __global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
 // GELU: 65 us, 3.1 TB/s).
 struct GradArgs {
     const void *Z, *dY;
-    void *G;                  // nullable, an operand of rows of pad8(N)
-    void *low;                // nullable: what the rounding of G to a 16-bit type left
+    void *G;                  // nullable, an operand of rows of pad8(N) elements, ldg apart
+    int64_t ldg, low;         // low: 0, or elements from G to what its rounding to a 16-bit type left
     float *col;               // nullable [chunks x N]
     void *db;                 // nullable [N], of a single chunk
     int64_t ldz, lddy, M, N, chunk;   // chunk: rows of a workgroup
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
     const int t = threadIdx.x;
     const int64_t c = ((int64_t)blockIdx.y * a.groups + t % a.groups) * 8;
     const int64_t r0 = (int64_t)blockIdx.x * a.chunk;
-    const int64_t r1 = r0 + a.chunk < a.M ? r0 + a.chunk : a.M, ldg = (a.N + 7) / 8 * 8;
+    const int64_t r1 = r0 + a.chunk < a.M ? r0 + a.chunk : a.M, padded = (a.N + 7) / 8 * 8;
     DropState st;
     if (a.drop.rng) st.init(a.drop, a.N);
     float sum[8] = {};
@@ -117,12 +120,15 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = c + j < a.N ? v[j] : 0.0f;
             }
-            if (a.G) store8((T *)a.G + r * ldg, c, ldg, v);
-            if (a.low) {
-                float w[8];
+            if (a.G) {
+                T *G = (T *)a.G + r * a.ldg;
+                store8(G, c, padded, v);
+                if (a.low) {
+                    float w[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
-                store8((T *)a.low + r * ldg, c, ldg, w);
+                    for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
+                    store8(G + a.low, c, padded, w);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -190,8 +196,12 @@ static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t 
            d_out <= LINEAR_MAX_WIDTH && max_rows >= 1 && max_rows <= MLP_MAX_BATCH;
 }
 
-// Workspace (ws null: its size alone): the operands g, X and W, the partial column sums, the
-// partial products, the arrival counts.
+// Whether a width is below what linear_skinny.hip takes.
+static bool any_narrow(const LinearCtx &c) { return c.d_in < SKINNY_WIDTH || c.d_out < SKINNY_WIDTH; }
+
+// Workspace (ws null: its size alone): the operands g, X and W (of 16-bit types with room for
+// the second values of g, and for X and W twice where narrow products need that), the partial
+// column sums, the partial products, the arrival counts.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -201,10 +211,11 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     };
     const size_t element = dtype_bytes(c->dtype);
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
-    c->g = take(element * M * pad8(N));
-    c->low = take(element == 2 ? element * (M < 64 ? M : 64) * pad8(N) : 0);
-    c->x = take(element * M * pad8(K));
-    c->w = take(element * K * pad8(N));
+    const int64_t more = element == 2 ? (M < REST_ROWS ? M : REST_ROWS) : 0;
+    const bool twice = element == 2 && any_narrow(*c);
+    c->g = take(element * (M + more) * pad8(N));
+    c->x = take(element * (M + (twice ? more : 0)) * pad8(K));
+    c->w = take(element * (twice ? 2 * K : K) * pad8(N));
     c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
     int64_t most = M * N > M * K ? M * N : M * K;
     if (most < K * N) most = K * N;
@@ -221,15 +232,17 @@ struct Operands {
     PackArgs a{};
     explicit Operands(const LinearCtx &ctx) : c(ctx) {}
     // The matrix [rows x cols] at P: as it is where its layout is an operand's (and its rows
-    // close enough for 32-bit offsets within a tile), else packed at `room` by launch().
+    // close enough for 32-bit offsets within a tile), else packed at `room` by launch(); twice:
+    // each row two times, packed.
     template <class T>
-    Operand get(const void *P, int64_t ld, int64_t rows, int64_t cols, void *room) {
+    Operand get(const void *P, int64_t ld, int64_t rows, int64_t cols, void *room, bool twice = false) {
         if (rows <= 1) ld = pad8(cols);
         const bool fits = sizeof(T) == 4 ? cols >= 4 : ((uintptr_t)P & 15u) == 0 && ld % 8 == 0 && cols % 8 == 0;
-        if (fits && ld < (1 << 22)) return Operand{P, ld, cols};
+        if (fits && ld < (1 << 22) && !twice) return Operand{P, ld, cols};
+        if (twice) rows *= 2;
         if (rows > 0) {
             const int64_t need = ceil_div(rows * (pad8(cols) / 8), 256);
-            a.job[a.jobs] = PackArgs::Job{P, room, ld, rows, cols};
+            a.job[a.jobs] = PackArgs::Job{P, room, ld, rows, cols, twice};
             a.groups[a.jobs] = (a.jobs ? a.groups[a.jobs - 1] : 0) + (need < 4096 ? need : 4096);
             ++a.jobs;
         }
@@ -252,7 +265,7 @@ struct Operands {
 // 1,024 x 1,024 16 and 15, 100 x 300 x 16,384 32 and 37; in bf16: 64 x 1,024 x 1,024 8.4 and 8.4,
 // 256 x 1,024 x 1,024 10.2 and 8.5, 100 x 30 x 10,001 14 and 28).
 static bool few_rows(const LinearCtx &c, int64_t M, bool back) {
-    if (c.d_in < SKINNY_WIDTH || c.d_out < SKINNY_WIDTH) return false;
+    if (any_narrow(c)) return false;
     const bool f32 = c.dtype == MLP_F32, deep = (back ? c.d_out : c.d_in) > 4096;
     const int64_t rows = back && !f32 && !deep ? 64 : FEW_ROWS;
     const int64_t size = !f32 ? 1 << 28 : deep ? 1 << 29 : back ? 1 << 27 : 1 << 28;
@@ -294,27 +307,38 @@ struct BackwardArgs {
 template <class T>
 static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     const int64_t M = b.rows, N = c.d_out, K = c.d_in;
-    const bool products = M > 0 && (b.dX || b.dW), few = few_rows(c, M, true);
-    // without activation and dropout g is dY, and dY itself the operand (of few rows, where
-    // 32-bit offsets reach over the depth of a step)
-    const bool same = c.act == MLP_ACT_NONE && !b.drop.rng && (!few || b.lddy < (1 << 24));
+    const bool products = M > 0 && (b.dX || b.dW), as_is = c.act == MLP_ACT_NONE && !b.drop.rng;
+    const bool few = few_rows(c, M, true);
     // The products take g rounded to a 16-bit type, a rounding more than their result's own.
     // Of up to 64 rows, where it would show (an element of g is in every value of a row of
-    // dX) and W or latency is the bound, what it left goes along as a second value.
-    const bool rest = sizeof(T) == 2 && few && M <= 64 && !same;
+    // dX) and W or latency is the bound, what it left goes along as a second value, behind
+    // the first ones of the row. It costs up to a few us (both gradients in bf16, us with
+    // and without: 64 x 4,096 x 1 16.8 and 16.6, 64 x 1 x 4,096 27.4 and 22.6, 64 x 7 x 1,000 22.0
+    // and 18.6), but for large products of 33 to 64 rows (64 x 4,096 x 4,096 50 and 35), which
+    // do without, as more rows do, whose matrix instructions would be twice as many (456 of
+    // the 530 us of 8,192 x 4,096 x 4,096, for an error of dX and dW of 1.65e-3, their own
+    // rounding's, in place of 2.34e-3).
+    const bool rest = sizeof(T) == 2 && M <= REST_ROWS && !as_is && (few || any_narrow(c));
+    // g that is dY itself: dY is the operand (of few rows, where 32-bit offsets reach over
+    // the depth of a step)
+    const bool same = as_is && (!few || b.lddy < (1 << 24));
     // what goes to linear_skinny.hip: dX of few_rows, and dW of 32 rows (us there and on
     // tiles, 4,096 x 4,096: bf16 12.5 and 14.6, fp32 33 and 33) or, for the second values, 64
-    const bool outer = few && M <= (sizeof(T) == 4 ? 32 : 64);
+    const bool outer = few && M <= (sizeof(T) == 4 ? 32 : REST_ROWS);
+    // Second values on tiles: (g, low) by (w, w) along the depth of dX, and by x in the row of
+    // g and in that of low for dW, whose rows alternate.
+    const bool twice = rest && !few;
+    const int64_t low = rest ? pad8(N) : 0, ldg = pad8(N) + low;
     Operands o(c);
-    Operand x{}, w{c.W, N, N}, g{c.g, pad8(N), pad8(N)};
+    Operand x{}, w{c.W, N, N}, g{c.g, ldg, ldg};
     if (same && products) {
         if (few && (outer || !b.dW)) g = Operand{b.dY, b.lddy, N};
         else g = o.get<T>(b.dY, b.lddy, M, N, c.g);
     }
     // (16-bit rows that start at odd elements load slowly: where many rows of g read W, it is
     // laid out first for k_skinny too: 700 x 30 x 10,001 in bf16 29 us, 20 so)
-    if (b.dX && M > 0 && (!few || (sizeof(T) == 2 && M > 128 && N % 2))) w = o.get<T>(c.W, N, K, N, c.w);
-    if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x);
+    if (b.dX && M > 0 && (!few || (sizeof(T) == 2 && M > 128 && N % 2))) w = o.get<T>(c.W, N, K, N, c.w, twice);
+    if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x, twice);
     if (hipError_t e = o.launch<T>()) return e;
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
@@ -331,7 +355,8 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.Z = b.Z;
         a.dY = b.dY;
         a.G = products && !same ? c.g : nullptr;
-        a.low = rest && a.G ? c.low : nullptr;
+        a.ldg = ldg;
+        a.low = low;
         a.col = b.db && chunks > 1 ? c.col : nullptr;
         a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
@@ -353,18 +378,19 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     if (b.dX && M > 0) {
         e.Y = b.dX;
         e.ldy = b.lddx;
+        if (twice) w.ld = w.len = ldg;
         const hipError_t s =
-            few ? launch_skinny(GEMM_NT, c.dtype, g.p, g.ld, rest ? (T *)c.low - (T *)c.g : 0, w.p, w.ld, M, K, N, e,
-                                c.part, c.part_floats, c.arrived, c.arrived_words, c.stream)
-                : launch_gemm(GEMM_NT, c.dtype, g, w, M, K, N, e, c.part, c.part_floats, c.stream);
+            few ? launch_skinny(GEMM_NT, c.dtype, g.p, g.ld, low, w.p, w.ld, M, K, N, e, c.part, c.part_floats, c.arrived,
+                                c.arrived_words, c.stream)
+                : launch_gemm(GEMM_NT, c.dtype, g, w, M, K, twice ? ldg : N, e, c.part, c.part_floats, c.stream);
         if (s != hipSuccess) return s;
     }
     if (!b.dW) return hipSuccess;
-    if (outer)
-        return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, rest ? (T *)c.low - (T *)c.g : 0, M, K, N, b.dW, c.stream);
+    if (outer) return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, low, M, K, N, b.dW, c.stream);
     e.Y = b.dW;
     e.ldy = N;
-    return launch_gemm(GEMM_TN, c.dtype, x, g, K, N, M, e, c.part, c.part_floats, c.stream);
+    if (twice) g.ld = g.len = low;
+    return launch_gemm(GEMM_TN, c.dtype, x, g, K, N, twice ? 2 * M : M, e, c.part, c.part_floats, c.stream);
 }
 
 __global__ __launch_bounds__(256) void k_clear(uint32_t *p, int64_t n) {
