@@ -405,6 +405,7 @@ mlp_status mlp_linear_forward(mlp_linear_t ctx, const void *X, int64_t ldx, int6
  * matrix cores take such operands): the error of dX and dW is then about sqrt(2) times that
  * of their own rounding. Not so for 32 rows or fewer, nor for up to 64 while rows d_in d_out
  * <= 2^28 or a width is below 8 (g comes as two values, down to the type's smallest step).
+ * In fp16 g is kept within the type's range by a power of two, so it is finite where dY is.
  * dbias is summed from the unrounded g.
  *   X      [rows x d_in] as in the forward call (used by dW only; may be NULL without)
  *   Z      [rows x d_out] from the forward call; NULL only if the activation is NONE

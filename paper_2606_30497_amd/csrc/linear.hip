@@ -5,6 +5,7 @@
 
 #include <new>
 #include <stdint.h>
+#include <type_traits>
 
 #include "layer.h"
 #include "linear_internal.h"
@@ -76,6 +77,7 @@ struct GradArgs {
     const void *Z, *dY;
     void *G;                  // nullable, an operand of rows of pad8(N) elements, ldg apart
     int64_t ldg, low;         // low: 0, or elements from G to what its rounding to a 16-bit type left
+    float shrink;             // what G holds is g times this (fp16; else 1)
     float *col;               // nullable [chunks x N]
     void *db;                 // nullable [N], of a single chunk
     int64_t ldz, lddy, M, N, chunk;   // chunk: rows of a workgroup
@@ -122,13 +124,21 @@ __global__ __launch_bounds__(256) void k_linear_grad(const GradArgs a) {
             }
             if (a.G) {
                 T *G = (T *)a.G + r * a.ldg;
-                store8(G, c, padded, v);
-                if (a.low) {
-                    float w[8];
+                float w[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = v[j] - up((T)v[j]);
-                    store8(G + a.low, c, padded, w);
+                for (int j = 0; j < 8; ++j) w[j] = std::is_same<T, f16>::value ? v[j] * a.shrink : v[j];
+                if (a.low) {   // (an infinity goes to the second value: of two, inf - inf would be left)
+                    constexpr float MOST = std::is_same<T, f16>::value ? 65504.0f : 3.38953139e38f;
+                    float rest[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float first = fminf(fmaxf(w[j], -MOST), MOST);
+                        rest[j] = w[j] - up((T)first);
+                        w[j] = first;
+                    }
+                    store8(G + a.low, c, padded, rest);
                 }
+                store8(G, c, padded, w);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -296,6 +306,17 @@ static hipError_t linear_forward(const LinearCtx &c, const void *X, int64_t ldx,
     return launch_gemm(GEMM_NN, c.dtype, x, w, rows, c.d_out, c.d_in, e, c.part, c.part_floats, c.stream);
 }
 
+// The power of two that |g| / |dY| stays below: fp16 has no room for a'(z) > 1 and dropout's
+// 1 / q next to a dY of a loss that was scaled up, so g is kept divided by this, and the sums
+// are multiplied with it. (The smallest step of g grows with it, to at most twice what dY's own
+// smallest step makes in g.)
+static float headroom(int act, const Drop &drop) {
+    const float most = (act == MLP_ACT_NONE || act == MLP_ACT_RELU ? 1.0f : 1.13f) * (drop.rng ? drop.scale : 1.0f);
+    float s = 1.0f;
+    while (s < most) s *= 2.0f;
+    return s;
+}
+
 struct BackwardArgs {
     const void *X, *Z, *dY;
     int64_t ldx, ldz, lddy, rows;
@@ -328,6 +349,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // Second values on tiles: (g, low) by (w, w) along the depth of dX, and by x in the row of
     // g and in that of low for dW, whose rows alternate.
     const bool twice = rest && !few;
+    const float scale = std::is_same<T, f16>::value && !as_is ? headroom(c.act, b.drop) : 1.0f;
     const int64_t low = rest ? pad8(N) : 0, ldg = pad8(N) + low;
     Operands o(c);
     Operand x{}, w{c.W, N, N}, g{c.g, ldg, ldg};
@@ -357,6 +379,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         a.G = products && !same ? c.g : nullptr;
         a.ldg = ldg;
         a.low = low;
+        a.shrink = 1.0f / scale;
         a.col = b.db && chunks > 1 ? c.col : nullptr;
         a.db = chunks == 1 ? b.db : nullptr;
         a.ldz = b.ldz;
@@ -375,6 +398,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         if (hipError_t e = hipGetLastError()) return e;
     }
     Epilogue e{};
+    e.scale = scale;
     if (b.dX && M > 0) {
         e.Y = b.dX;
         e.ldy = b.lddx;
@@ -386,7 +410,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
         if (s != hipSuccess) return s;
     }
     if (!b.dW) return hipSuccess;
-    if (outer) return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, low, M, K, N, b.dW, c.stream);
+    if (outer) return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, low, M, K, N, scale, b.dW, c.stream);
     e.Y = b.dW;
     e.ldy = N;
     if (twice) g.ld = g.len = low;

@@ -10,9 +10,10 @@
 
 namespace mlp {
 
-// What becomes of the fp32 sums of a matrix product: Y = R + dropout(a(sum + bias)),
-// Z = sum + bias; everything but Y may be missing.
+// What becomes of the fp32 sums of a matrix product: Y = R + dropout(a(scale sum + bias)),
+// Z = scale sum + bias; everything but Y may be missing.
 struct Epilogue {
+    float scale = 1.0f;   // a power of two
     const void *bias, *R;
     void *Z, *Y;
     int64_t ldr, ldz, ldy;
@@ -35,6 +36,10 @@ struct Finish {
     // v: the sums of row r; res: the row's residual
     __device__ __forceinline__ void finish(const Epilogue &e, int64_t r, int64_t c, int64_t n, float (&v)[8],
                                            const Oct<T> &res) const {
+        if (e.scale != 1.0f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= e.scale;
+        }
         if (e.bias) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += bias[j];
@@ -96,9 +101,9 @@ hipError_t launch_skinny(int op, int32_t dtype, const void *X, int64_t ldx, int6
 // Y = X W of N < SKINNY_WIDTH outputs
 hipError_t launch_narrow(int32_t dtype, const void *X, int64_t ldx, const void *W, int64_t M, int64_t N, int64_t K,
                          const Epilogue &e, hipStream_t stream);
-// dW [K x N] = X^T G of M rows, N >= SKINNY_WIDTH; low as above, of G
+// dW [K x N] = scale X^T G of M rows, N >= SKINNY_WIDTH; low as above, of G
 hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t low,
-                        int64_t M, int64_t K, int64_t N, void *dW, hipStream_t stream);
+                        int64_t M, int64_t K, int64_t N, float scale, void *dW, hipStream_t stream);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

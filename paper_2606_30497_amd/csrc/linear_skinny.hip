@@ -374,6 +374,7 @@ struct OuterArgs {
     int64_t low;   // LOW: elements from G to what its rounding left
     int64_t ldx, ldg, M, K, N;
     int tiles;     // tiles of 16 k a wave
+    float scale;   // of the sums
 };
 
 template <class T, bool LOW, bool EDGE>
@@ -420,7 +421,7 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int64_t k0, int64_t n0
                 const int64_t n = n0 + 8 * (4 * v + (lane >> 4));
                 float w[8];
 #pragma unroll
-                for (int t = 0; t < 8; ++t) w[t] = acc[0][t][v];
+                for (int t = 0; t < 8; ++t) w[t] = acc[0][t][v] * a.scale;
                 if (n < a.N) store8((T *)a.dW + k * a.N, n, a.N, w);
             }
         }
@@ -436,10 +437,10 @@ __global__ __launch_bounds__(256) void k_outer(const OuterArgs a) {
 }
 
 hipError_t launch_outer(int32_t dtype, const void *X, int64_t ldx, const void *G, int64_t ldg, int64_t low,
-                        int64_t M, int64_t K, int64_t N, void *dW, hipStream_t stream) {
+                        int64_t M, int64_t K, int64_t N, float scale, void *dW, hipStream_t stream) {
     // about 1,024 workgroups of four waves
     const int64_t across = ceil_div(N, SKINNY_N), tiles = ceil_div(ceil_div(K, 64) * across, 1024);
-    const OuterArgs a{X, G, dW, low, ldx, ldg, M, K, N, (int)(tiles < 16 ? tiles : 16)};
+    const OuterArgs a{X, G, dW, low, ldx, ldg, M, K, N, (int)(tiles < 16 ? tiles : 16), scale};
     const dim3 grid((unsigned)across, (unsigned)ceil_div(K, 64 * a.tiles));
 #define OUTER(T, LOW) hipLaunchKernelGGL((k_outer<T, LOW>), grid, dim3(256), 0, stream, a)
     switch (dtype) {
