@@ -527,6 +527,11 @@ class LinearContext:
             _lib.mlp_linear_destroy(h)
 
 
+def _stream(handle, device):
+    """The stream of a handle; 0 is the device's default stream."""
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
 def mlp_linear_workspace_bytes(dtype: torch.dtype, d_in: int, d_out: int, max_rows: int) -> int:
     return int(load().mlp_linear_workspace_bytes(DTYPES[dtype], d_in, d_out, max_rows))
 
@@ -579,9 +584,7 @@ def _bind_stream(ctx):
     now = _current_stream(ctx.device.index)
     if now != ctx.bound:
         if not torch.cuda.is_current_stream_capturing():
-            before = (torch.cuda.ExternalStream(ctx.bound, device=ctx.device) if ctx.bound
-                      else torch.cuda.default_stream(ctx.device))
-            torch.cuda.current_stream(ctx.device).wait_stream(before)
+            torch.cuda.current_stream(ctx.device).wait_stream(_stream(ctx.bound, ctx.device))
         _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
         ctx.bound = now
 
@@ -590,7 +593,7 @@ def _new(ctx, *shape):
     """An output of the context's type, its memory taken on the stream that writes it."""
     if ctx.stream is None:
         return torch.empty(shape, dtype=ctx.dtype, device=ctx.device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.device)):
+    with torch.cuda.stream(_stream(ctx.stream, ctx.device)):
         return torch.empty(shape, dtype=ctx.dtype, device=ctx.device)
 
 

@@ -1,0 +1,109 @@
+"""Which streams the binding of the dense layer allocates on, waits for and reports to the
+allocator, on stand-ins for torch's streams and memory (no GPU)."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+from paper_2606_30497_amd import mlp
+
+
+class Stream:
+    def __init__(self, world, handle):
+        self.world, self.cuda_stream = world, handle
+
+    def wait_stream(self, other):
+        self.world.log.append(("wait", self.cuda_stream, other.cuda_stream))
+
+
+class Memory:
+    """What torch.empty gives: the stream whose pool it is from, and those it was told of."""
+
+    def __init__(self, world, shape, dtype=torch.float32):
+        self.world, self.shape, self.dtype = world, shape, dtype
+        self.device, self.pool, self.recorded = types.SimpleNamespace(index=0), world.current, set()
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return 1 << 20
+
+    def data_ptr(self):
+        return 4096
+
+    def record_stream(self, s):
+        self.recorded.add(s.cuda_stream)
+
+
+class World:
+    """torch.cuda of one device: 0 is its default stream, a stream made of the handle 0 is a
+    new one (as torch's are), `capturing` the handles of streams that capture."""
+
+    def __init__(self):
+        self.current, self.capturing, self.log = 0, set(), []
+        self.device = lambda device: contextlib.nullcontext()
+
+    def ExternalStream(self, handle, device=None):
+        return Stream(self, handle or 9999)
+
+    def default_stream(self, device=None):
+        return Stream(self, 0)
+
+    def current_stream(self, device=None):
+        return Stream(self, self.current)
+
+    def is_current_stream_capturing(self):
+        return self.current in self.capturing
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        before, self.current = self.current, s.cuda_stream
+        yield
+        self.current = before
+
+
+class Lib:
+    """The library: where its context is."""
+
+    def __init__(self, world):
+        self.world, self.on = world, None
+
+    def mlp_linear_workspace_bytes(self, *a):
+        return 4096
+
+    def mlp_linear_init(self, *a):
+        self.on = a[-1]
+        self.world.log.append(("clear", a[-1]))
+        return 0
+
+    def mlp_linear_set_stream(self, handle, stream):
+        self.on = stream
+        return 0
+
+
+@pytest.fixture
+def world(monkeypatch):
+    w = World()
+    lib = Lib(w)
+    w.lib = lib
+    fake = types.SimpleNamespace(cuda=w, uint8=torch.uint8, Tensor=torch.Tensor,
+                                 empty=lambda shape, dtype, device: Memory(w, shape, dtype))
+    monkeypatch.setattr(mlp, "torch", fake)
+    monkeypatch.setattr(mlp, "load", lambda: lib)
+    monkeypatch.setattr(mlp, "_lib", None)
+    monkeypatch.setattr(mlp, "_dev", lambda t, *a, **k: t.data_ptr())
+    monkeypatch.setattr(mlp, "_current_stream", lambda index: w.current)
+    return w
+
+
+def _layer(world, **k):
+    return mlp.mlp_linear_init(Memory(world, (16, 24)), None, "none", max_rows=8, **k)
+
+
+def test_the_default_stream_given_by_its_handle(world):
+    """Outputs of a context on the stream 0 are from the default stream's pool."""
+    ctx = _layer(world, stream=0)
+    world.current = 5
+    assert mlp._new(ctx, 8, 24).pool == 0
