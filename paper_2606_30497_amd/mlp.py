@@ -540,7 +540,9 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
                     stream=None) -> LinearContext:
     """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
     bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS. Calls
-    go on `stream`, or on the current stream at each call where none is given."""
+    go on `stream`, or on the current stream at each call where none is given; a caller's
+    workspace is taken to be free there. A HIP graph that holds calls replays them on the
+    context's workspace: keep the context as long as the graph."""
     lib = load()
     if W.dim() != 2:
         raise ValueError("W must be [d_in, d_out]")
@@ -553,12 +555,13 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
     if need == 0:
         raise MLPError("mlp_linear_workspace_bytes", -2)
     with torch.cuda.device(W.device):
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=W.device)
+        bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
+        if workspace is None:   # its memory in the order of the stream that clears and uses it
+            with torch.cuda.stream(_stream(bound, W.device)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=W.device)
         if workspace.device != W.device:
             raise ValueError("workspace is on %s, not on %s" % (workspace.device, W.device))
         _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
-        bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
         handle = _vp()
         _check("mlp_linear_init",
                lib.mlp_linear_init(ctypes.byref(handle), DTYPES[W.dtype], d_in, d_out,
@@ -568,11 +571,20 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
 
 
 def mlp_linear_set_stream(ctx: LinearContext, stream) -> None:
-    """Later calls go on `stream` (None: on the current stream at each call)."""
+    """Later calls go on `stream` (None: on the current stream at each call). The stream has
+    to live as long as the context."""
     if stream is not None:
-        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, stream))
-        ctx.bound = stream
+        _move(ctx, stream)
     ctx.stream = stream
+
+
+def _move(ctx, now):
+    """Put the context on the stream `now`. When the context is dropped, maybe with calls
+    under way, its workspace goes back to the allocator, which has to know of every stream
+    that it was used on."""
+    ctx.workspace.record_stream(_stream(now, ctx.device))
+    _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
+    ctx.bound = now
 
 
 def _bind_stream(ctx):
@@ -585,8 +597,7 @@ def _bind_stream(ctx):
     if now != ctx.bound:
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(ctx.device).wait_stream(_stream(ctx.bound, ctx.device))
-        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
-        ctx.bound = now
+        _move(ctx, now)
 
 
 def _new(ctx, *shape):

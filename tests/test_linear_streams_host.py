@@ -107,3 +107,30 @@ def test_the_default_stream_given_by_its_handle(world):
     ctx = _layer(world, stream=0)
     world.current = 5
     assert mlp._new(ctx, 8, 24).pool == 0
+
+
+def test_workspace_is_from_the_pool_of_the_stream_that_clears_it(world):
+    """What is pending on the current stream may still write to the block that its pool gives:
+    the clear of the arrival counts on another stream would not come after it."""
+    world.current = 5
+    for given, pool in ((None, 5), (7, 7), (0, 0)):
+        ctx = _layer(world, stream=given)
+        assert ctx.workspace.pool == pool and world.log[-1] == ("clear", pool)
+
+
+def test_allocator_knows_the_streams_of_the_workspace(world):
+    """A context made on one stream and called on others gives its workspace back to the
+    first one's pool: only what the allocator was told of keeps it from the next tensor."""
+    world.current = 5
+    ctx = _layer(world)
+    for s in (5, 6, 5, 0):
+        world.current = s
+        mlp._bind_stream(ctx)
+        assert world.lib.on == s
+    mlp.mlp_linear_set_stream(ctx, 8)
+    assert ctx.workspace.recorded | {5} == {5, 6, 0, 8}
+    own = _layer(world, stream=7)
+    mlp.mlp_linear_set_stream(own, None)
+    world.current = 6
+    mlp._bind_stream(own)
+    assert own.workspace.recorded | {7} == {7, 6}
