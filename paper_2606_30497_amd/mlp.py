@@ -520,6 +520,7 @@ class LinearContext:
         self.activation, self.max_rows = activation, max_rows
         self.stream = stream    # None: each call goes on the current stream
         self.bound = bound      # the stream the library's context is on
+        self.last = bound       # the stream of the last call that was not captured
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -571,33 +572,37 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
 
 
 def mlp_linear_set_stream(ctx: LinearContext, stream) -> None:
-    """Later calls go on `stream` (None: on the current stream at each call). The stream has
-    to live as long as the context."""
+    """Later calls go on `stream` (None: on the current stream at each call), behind those
+    before. The stream has to live as long as the context."""
     if stream is not None:
         _move(ctx, stream)
     ctx.stream = stream
 
 
 def _move(ctx, now):
-    """Put the context on the stream `now`. When the context is dropped, maybe with calls
-    under way, its workspace goes back to the allocator, which has to know of every stream
-    that it was used on."""
-    ctx.workspace.record_stream(_stream(now, ctx.device))
-    _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
-    ctx.bound = now
+    """Put the context on the stream `now`, behind the calls it made on another one before
+    (a stream that captures cannot wait for those: there the capture's own start has to be
+    behind them, and the next call that is not captured still waits). When the context is
+    dropped, maybe with calls under way, its workspace goes back to the allocator, which has
+    to know of every stream that it was used on."""
+    at = _stream(now, ctx.device)
+    with torch.cuda.device(ctx.device), torch.cuda.stream(at):
+        captured = torch.cuda.is_current_stream_capturing()
+    if now != ctx.last and not captured:
+        at.wait_stream(_stream(ctx.last, ctx.device))
+        ctx.last = now
+    if now != ctx.bound:
+        ctx.workspace.record_stream(at)
+        _check("mlp_linear_set_stream", load().mlp_linear_set_stream(ctx.handle, now))
+        ctx.bound = now
 
 
 def _bind_stream(ctx):
-    """Put the context on the current stream where it has none of its own, behind the
-    calls it made on another one before (a stream that captures cannot wait for those:
-    there the capture's own start has to be behind them)."""
-    if ctx.stream is not None:
-        return
-    now = _current_stream(ctx.device.index)
-    if now != ctx.bound:
-        if not torch.cuda.is_current_stream_capturing():
-            torch.cuda.current_stream(ctx.device).wait_stream(_stream(ctx.bound, ctx.device))
-        _move(ctx, now)
+    """Put the context on the current stream where it has none of its own."""
+    if ctx.stream is None:
+        now = _current_stream(ctx.device.index)
+        if now != ctx.bound or now != ctx.last:
+            _move(ctx, now)
 
 
 def _new(ctx, *shape):

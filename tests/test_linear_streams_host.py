@@ -134,3 +134,37 @@ def test_allocator_knows_the_streams_of_the_workspace(world):
     world.current = 6
     mlp._bind_stream(own)
     assert own.workspace.recorded | {7} == {7, 6}
+
+
+def test_calls_wait_for_those_before_them(world):
+    """Each call that is not captured waits for the last one that was not, whose workspace it
+    shares; a capture on another stream in between changes nothing in that."""
+    world.current = 5
+    ctx = _layer(world)
+    del world.log[:]
+
+    def call(stream, *waits):
+        world.current = stream
+        mlp._bind_stream(ctx)
+        assert world.lib.on == stream and world.log == list(waits), (stream, world.log)
+        del world.log[:]
+
+    call(5)
+    call(6, ("wait", 6, 5))
+    call(6)
+    world.capturing = {7}
+    call(7)                       # recorded, not run: nothing to wait for or to be waited for
+    call(7)
+    call(8, ("wait", 8, 6))       # while 7 still captures: an event of 7 would draw 8 into the capture
+    call(7)
+    world.capturing = set()
+    call(7, ("wait", 7, 8))       # the library's context is on 7 already
+    call(0, ("wait", 0, 7))
+    mlp.mlp_linear_set_stream(ctx, 9)
+    assert world.log == [("wait", 9, 0)] and world.lib.on == 9
+    del world.log[:]
+    world.current = 5
+    mlp._bind_stream(ctx)         # a stream of its own: the current one does not matter
+    assert world.log == [] and world.lib.on == 9
+    mlp.mlp_linear_set_stream(ctx, None)
+    call(5, ("wait", 5, 9))
