@@ -148,6 +148,18 @@ def _dev(t, name, dtype=torch.float32, numel=None):
     return t.data_ptr()
 
 
+def _stream(handle, device):
+    """The stream of a handle; 0 is the device's default stream."""
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
+def _workspace(need, device, stream):
+    """A workspace whose memory is in the order of the stream that clears and uses it: what is
+    pending on another one may still write to a block of that one's pool."""
+    with torch.cuda.stream(_stream(stream, device)):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
 def mlp_workspace_bytes(d_in: int, hidden: int, max_batch: int) -> int:
     return int(load().mlp_workspace_bytes(d_in, hidden, max_batch))
 
@@ -155,9 +167,10 @@ def mlp_workspace_bytes(d_in: int, hidden: int, max_batch: int) -> int:
 class Context:
     """A library context bound to caller-owned W1, W2 and workspace tensors."""
 
-    def __init__(self, handle, W1, W2, workspace, max_batch):
+    def __init__(self, handle, W1, W2, workspace, max_batch, stream):
         self.handle = handle
         self.W1, self.W2, self.workspace = W1, W2, workspace
+        self.stream = stream
         self.max_batch = max_batch
         self.hidden = W1.shape[1]
         self.strategy_workspace = None
@@ -180,20 +193,26 @@ def mlp_init(W1: torch.Tensor, W2: torch.Tensor, max_batch: int, workspace=None,
     need = lib.mlp_workspace_bytes(d_in, h, max_batch)
     if need == 0:
         raise MLPError("mlp_workspace_bytes", -2)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=W1.device)
-    _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
     if stream is None:
         stream = torch.cuda.current_stream(W1.device).cuda_stream
+    if workspace is None:
+        workspace = _workspace(need, W1.device, stream)
+    _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
     handle = _vp()
     _check("mlp_init", lib.mlp_init(ctypes.byref(handle), d_in, h, 1, max_batch, W1.data_ptr(),
                                     W2.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                     stream))
-    return Context(handle, W1, W2, workspace, max_batch)
+    return Context(handle, W1, W2, workspace, max_batch, stream)
 
 
 def mlp_set_stream(ctx: Context, stream) -> None:
+    """Later calls go on `stream`, which the caller orders behind those before; it has to
+    live as long as the context."""
     _check("mlp_set_stream", load().mlp_set_stream(ctx.handle, stream))
+    ctx.stream = stream
+    for w in (ctx.workspace, ctx.strategy_workspace):
+        if w is not None:   # the allocator has to know of every stream that it was used on
+            w.record_stream(_stream(stream, w.device))
 
 
 def mlp_strategy_workspace_bytes(d_in: int, hidden: int, max_batch: int, strategy: int) -> int:
@@ -206,7 +225,7 @@ def mlp_set_strategy(ctx: Context, strategy, workspace=None) -> None:
     code = STRATEGIES[strategy] if isinstance(strategy, str) else int(strategy)
     need = mlp_strategy_workspace_bytes(D_IN, ctx.hidden, ctx.max_batch, code)
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=ctx.W1.device)
+        workspace = _workspace(need, ctx.W1.device, ctx.stream)
     ptr = _dev(workspace, "workspace", dtype=torch.uint8, numel=need) if workspace is not None else None
     nbytes = workspace.numel() if workspace is not None else 0
     _check("mlp_set_strategy", load().mlp_set_strategy(ctx.handle, code, ptr, nbytes))
@@ -377,11 +396,11 @@ def mlp_deep_init(params: torch.Tensor, hidden: int, layers: int, max_batch: int
     need = lib.mlp_deep_workspace_bytes(D_IN, hidden, layers, max_batch)
     if need == 0:
         raise MLPError("mlp_deep_workspace_bytes", -1)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=params.device)
-    _dev(workspace, "workspace", dtype=torch.uint8)
     if stream is None:
         stream = torch.cuda.current_stream(params.device).cuda_stream
+    if workspace is None:
+        workspace = _workspace(need, params.device, stream)
+    _dev(workspace, "workspace", dtype=torch.uint8)
     handle = _vp()
     # the library also takes a workspace without the part its panel path uses
     status = lib.mlp_deep_init(ctypes.byref(handle), D_IN, hidden, layers, 1, max_batch,
@@ -528,11 +547,6 @@ class LinearContext:
             _lib.mlp_linear_destroy(h)
 
 
-def _stream(handle, device):
-    """The stream of a handle; 0 is the device's default stream."""
-    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
-
-
 def mlp_linear_workspace_bytes(dtype: torch.dtype, d_in: int, d_out: int, max_rows: int) -> int:
     return int(load().mlp_linear_workspace_bytes(DTYPES[dtype], d_in, d_out, max_rows))
 
@@ -557,9 +571,8 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
         raise MLPError("mlp_linear_workspace_bytes", -2)
     with torch.cuda.device(W.device):
         bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
-        if workspace is None:   # its memory in the order of the stream that clears and uses it
-            with torch.cuda.stream(_stream(bound, W.device)):
-                workspace = torch.empty(need, dtype=torch.uint8, device=W.device)
+        if workspace is None:
+            workspace = _workspace(need, W.device, bound)
         if workspace.device != W.device:
             raise ValueError("workspace is on %s, not on %s" % (workspace.device, W.device))
         _dev(workspace, "workspace", dtype=torch.uint8, numel=need)

@@ -168,3 +168,23 @@ def test_calls_wait_for_those_before_them(world):
     assert world.log == [] and world.lib.on == 9
     mlp.mlp_linear_set_stream(ctx, None)
     call(5, ("wait", 5, 9))
+
+
+def test_workspaces_of_the_whole_nets(world):
+    """The same for mlp_init, mlp_set_strategy and mlp_deep_init, whose calls all go on the
+    context's own stream."""
+    lib, world.current = world.lib, 5
+    for name in ("mlp_workspace_bytes", "mlp_strategy_workspace_bytes", "mlp_deep_workspace_bytes", "mlp_deep_param_count"):
+        setattr(lib, name, lambda *a: 4096)
+    for name in ("mlp_init", "mlp_set_stream", "mlp_set_strategy", "mlp_deep_init"):
+        setattr(lib, name, lambda *a: 0)
+    w = Memory(world, (32, 64))
+    for given, pool in ((None, 5), (7, 7), (0, 0)):
+        ctx = mlp.mlp_init(w, w, 64, stream=given)
+        mlp.mlp_set_strategy(ctx, "tile")
+        assert ctx.workspace.pool == ctx.strategy_workspace.pool == pool
+        assert mlp.mlp_deep_init(w, 64, 2, 64, stream=given).workspace.pool == pool
+        mlp.mlp_set_stream(ctx, 8)
+        assert ctx.workspace.recorded == ctx.strategy_workspace.recorded == {8}
+        mlp.mlp_set_strategy(ctx, "baseline")
+        assert ctx.strategy_workspace.pool == 8
