@@ -651,7 +651,8 @@ def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, ou
 def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need_dx=True, need_dw=True,
                         need_db=True, dX=None, dW=None, db=None):
     """(dX, dW, db) of a forward call with the same X, p and rng; None for what is not
-    needed (db: for a layer without bias). X may be None where dW is not needed."""
+    needed (db: for a layer without bias). X may be None where dW is not needed. A dW of the
+    caller's is [d_in, d_out] or flat."""
     if dY.dim() != 2:
         raise ValueError("dY must be [rows, d_out]")
     rows, n, dev, dt = dY.shape[0], ctx.d_out, ctx.device, ctx.dtype
@@ -667,6 +668,8 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
         db = _new(ctx, n)
     dxp, lddx = _mat(dX, "dX", dt, dev, rows, ctx.d_in)
     dwp = _vec(dW, "dW", dt, dev, ctx.d_in * n)
+    if dW is not None and dW.dim() != 1 and dW.shape != (ctx.d_in, n):   # (flat: a slice of a bucket)
+        raise ValueError("dW must be [%d, %d], is %s" % (ctx.d_in, n, list(dW.shape)))
     dbp = _vec(db, "db", dt, dev, n)
     _bind_stream(ctx)
     _check("mlp_linear_backward",
