@@ -3,6 +3,7 @@
 // for any widths, row strides and the three types of mlp_dtype.
 #include <hip/hip_runtime.h>
 
+#include <initializer_list>
 #include <new>
 #include <stdint.h>
 #include <type_traits>
@@ -17,7 +18,9 @@ constexpr int COL_CHUNKS = 256;                   // most row chunks of the colu
 constexpr int64_t ARRIVED_WORDS = 16384;
 constexpr int64_t FEW_ROWS = 2048;                // most rows of a small product (few_rows)
 constexpr int64_t REST_ROWS = 64;                 // most rows whose g comes in two 16-bit values (linear_backward)
-constexpr int64_t PART_FLOATS_MAX = 256 * 65536;  // 256 workgroups' tiles of partial sums
+constexpr int64_t TILE_ROWS = 32;                 // up to here, at widths of eight and more, no tiles at all
+constexpr int64_t PART_TILES = 256 * 128 * 128;   // partial sums of 256 workgroups' split tiles, 128 x 128 at most
+constexpr int64_t PART_FEW = 256 * 32 * 128;      // and of k_skinny's 256 workgroups
 
 struct LinearCtx {
     int32_t dtype = 0, act = 0;
@@ -26,7 +29,7 @@ struct LinearCtx {
     // workspace: operands as the matrix products take them (Operand): the gradient in z,
     // and X and W where the caller's are not laid out so
     void *g = nullptr, *x = nullptr, *w = nullptr;
-    float *col = nullptr;       // [COL_CHUNKS x d_out], partial column sums of g
+    float *col = nullptr;       // [grad_chunks x d_out], partial column sums of g
     float *part = nullptr;      // partial sums of the products
     int64_t part_floats = 0;
     uint32_t *arrived = nullptr;   // the few-row products' arrival counts, zero between calls
@@ -209,9 +212,32 @@ static bool linear_shape_ok(int32_t dtype, int64_t d_in, int64_t d_out, int64_t 
 // Whether a width is below what linear_skinny.hip takes.
 static bool any_narrow(const LinearCtx &c) { return c.d_in < SKINNY_WIDTH || c.d_out < SKINNY_WIDTH; }
 
+// Columns of a workgroup of k_linear_grad, in eights (few rows: as many rows at a time as there
+// are, and fewer columns), and the most chunks of rows it takes a call's in: about four
+// workgroups a compute unit; up to 64 rows in one chunk, which gives db by itself.
+static int grad_groups(int64_t M, int64_t N) {
+    const int most = M > 32 && M <= 64 ? 4 : M > 16 && M <= 32 ? 8 : M > 8 && M <= 16 ? 16 : 32;
+    int groups = 1;
+    while (groups < most && groups * 8 < N) groups *= 2;
+    return groups;
+}
+static int64_t grad_chunks(int64_t M, int64_t N) {
+    if (M <= 64) return 1;
+    const int64_t want = ceil_div(1024, ceil_div(N, 8 * grad_groups(M, N)));
+    return want < COL_CHUNKS ? want : COL_CHUNKS;
+}
+
+// Floats that the partial sums of a product of M x N outputs take at most: splits of a depth
+// of 128 at least (four chunks of a tile, or a step of the eight waves of k_skinny, whose
+// rows of outputs are whole tiles), for up to 256 workgroups (512 of 64 x 64 tiles).
+static int64_t part_room(int64_t M, int64_t N, int64_t depth, int64_t most) {
+    const int64_t splits = ceil_div(depth, 128), all = M * (ceil_div(N, 128) * 128) * splits;
+    return splits <= 1 ? 0 : all < most ? all : most;
+}
+
 // Workspace (ws null: its size alone): the operands g, X and W (of 16-bit types with room for
-// the second values of g, and for X and W twice where narrow products need that), the partial
-// column sums, the partial products, the arrival counts.
+// the second values of g, and for X and W twice where narrow products need that; X and W only
+// where there are tiles), the partial column sums, the partial products, the arrival counts.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -224,12 +250,14 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const int64_t more = element == 2 ? (M < REST_ROWS ? M : REST_ROWS) : 0;
     const bool twice = element == 2 && any_narrow(*c);
     c->g = take(element * (M + more) * pad8(N));
-    c->x = take(element * (M + (twice ? more : 0)) * pad8(K));
-    c->w = take(element * (twice ? 2 * K : K) * pad8(N));
-    c->col = (float *)take(sizeof(float) * COL_CHUNKS * (size_t)N);
-    int64_t most = M * N > M * K ? M * N : M * K;
-    if (most < K * N) most = K * N;
-    c->part_floats = most < PART_FLOATS_MAX / 256 ? 256 * most : PART_FLOATS_MAX;
+    const bool tiles = M > TILE_ROWS || any_narrow(*c);
+    c->x = take(tiles ? element * (M + (twice ? more : 0)) * pad8(K) : 0);
+    c->w = take(tiles ? element * (twice ? 2 * K : K) * pad8(N) : 0);
+    c->col = (float *)take(M > 64 ? sizeof(float) * grad_chunks(M, N) * (size_t)N : 0);
+    c->part_floats = 0;
+    const int64_t most = tiles ? PART_TILES : PART_FEW;
+    for (const int64_t n : {part_room(M, N, K, most), part_room(M, K, N, most), part_room(K, N, M, most)})
+        if (n > c->part_floats) c->part_floats = n;
     c->part = (float *)take(sizeof(float) * (size_t)c->part_floats);
     c->arrived_words = ARRIVED_WORDS;
     c->arrived = (uint32_t *)take(sizeof(uint32_t) * (size_t)c->arrived_words);
@@ -279,7 +307,7 @@ static bool few_rows(const LinearCtx &c, int64_t M, bool back) {
     const bool f32 = c.dtype == MLP_F32, deep = (back ? c.d_out : c.d_in) > 4096;
     const int64_t rows = back && !f32 && !deep ? 64 : FEW_ROWS;
     const int64_t size = !f32 ? 1 << 28 : deep ? 1 << 29 : back ? 1 << 27 : 1 << 28;
-    return M <= (f32 ? 64 : 32) || (M <= rows && M * c.d_in * c.d_out <= size);
+    return M <= (f32 ? 64 : TILE_ROWS) || (M <= rows && M * c.d_in * c.d_out <= size);
 }
 
 // Whether y of fewer than eight outputs goes to k_narrow (us there and on tiles, rows x depth x
@@ -345,7 +373,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     const bool same = as_is && (!few || b.lddy < (1 << 24));
     // what goes to linear_skinny.hip: dX of few_rows, and dW of 32 rows (us there and on
     // tiles, 4,096 x 4,096: bf16 12.5 and 14.6, fp32 33 and 33) or, for the second values, 64
-    const bool outer = few && M <= (sizeof(T) == 4 ? 32 : REST_ROWS);
+    const bool outer = few && M <= (sizeof(T) == 4 ? TILE_ROWS : REST_ROWS);
     // Second values on tiles: (g, low) by (w, w) along the depth of dX, and by x in the row of
     // g and in that of low for dW, whose rows alternate.
     const bool twice = rest && !few;
@@ -365,14 +393,9 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
         GradArgs a;
-        // few rows: as many rows at a time as there are, and fewer columns
-        const int most = M > 32 && M <= 64 ? 4 : M > 16 && M <= 32 ? 8 : M > 8 && M <= 16 ? 16 : 32;
-        a.groups = 1;
-        while (a.groups < most && a.groups * 8 < N) a.groups *= 2;
+        a.groups = grad_groups(M, N);
         const int64_t step = 256 / a.groups;
-        // about four workgroups a compute unit; few rows in one chunk, which gives db
-        const int64_t want = ceil_div(1024, ceil_div(N, 8 * a.groups));
-        a.chunk = M <= 64 ? M : ceil_div(ceil_div(M, want < COL_CHUNKS ? want : COL_CHUNKS), step) * step;
+        a.chunk = M <= 64 ? M : ceil_div(ceil_div(M, grad_chunks(M, N)), step) * step;
         chunks = ceil_div(M, a.chunk);
         a.Z = b.Z;
         a.dY = b.dY;
