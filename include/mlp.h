@@ -375,7 +375,9 @@ size_t mlp_linear_workspace_bytes(int32_t dtype, int64_t d_in, int64_t d_out, in
  *   W           [d_in x d_out] contiguous, rows = inputs; read by every call
  *   bias        nullable [d_out]
  *   workspace   device buffer of at least mlp_linear_workspace_bytes bytes, 256-byte
- *               aligned, kept alive for the life of the context
+ *               aligned, kept alive for the life of the context; contexts may share
+ *               one, large enough for each, where none of their calls (this one among
+ *               them) and replays overlap
  *   stream      hipStream_t of that device to enqueue on (NULL = the null stream)
  * Enqueues a clear of the workspace's control words on `stream`; later calls must be
  * ordered after it (same stream, or a synchronisation), and after one another: calls on

@@ -235,9 +235,11 @@ static int64_t part_room(int64_t M, int64_t N, int64_t depth, int64_t most) {
     return splits <= 1 ? 0 : all < most ? all : most;
 }
 
-// Workspace (ws null: its size alone): the operands g, X and W (of 16-bit types with room for
-// the second values of g, and for X and W twice where narrow products need that; X and W only
-// where there are tiles), the partial column sums, the partial products, the arrival counts.
+// Workspace (ws null: its size alone): the arrival counts, at the start and as many whatever
+// the shape, so that contexts may share it (what else is there no call keeps); the operands g,
+// X and W (of 16-bit types with room for the second values of g, and for X and W twice where
+// narrow products need that; X and W only where there are tiles), the partial column sums, the
+// partial products.
 static size_t linear_carve(LinearCtx *c, char *ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -249,6 +251,8 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
     const int64_t more = element == 2 ? (M < REST_ROWS ? M : REST_ROWS) : 0;
     const bool twice = element == 2 && any_narrow(*c);
+    c->arrived_words = ARRIVED_WORDS;
+    c->arrived = (uint32_t *)take(sizeof(uint32_t) * (size_t)c->arrived_words);
     c->g = take(element * (M + more) * pad8(N));
     const bool tiles = M > TILE_ROWS || any_narrow(*c);
     c->x = take(tiles ? element * (M + (twice ? more : 0)) * pad8(K) : 0);
@@ -259,8 +263,6 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     for (const int64_t n : {part_room(M, N, K, most), part_room(M, K, N, most), part_room(K, N, M, most)})
         if (n > c->part_floats) c->part_floats = n;
     c->part = (float *)take(sizeof(float) * (size_t)c->part_floats);
-    c->arrived_words = ARRIVED_WORDS;
-    c->arrived = (uint32_t *)take(sizeof(uint32_t) * (size_t)c->arrived_words);
     return at;
 }
 

@@ -556,7 +556,8 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
     """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
     bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS. Calls
     go on `stream`, or on the current stream at each call where none is given; a caller's
-    workspace is taken to be free there. A HIP graph that holds calls replays them on the
+    workspace is taken to be free there (several layers may share one, if their calls do
+    not overlap: over streams the caller orders those). A HIP graph that holds calls replays them on the
     context's workspace: keep the context as long as the graph."""
     lib = load()
     if W.dim() != 2:

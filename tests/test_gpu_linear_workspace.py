@@ -68,3 +68,30 @@ def test_made_on_a_stream_of_its_own_while_another_is_busy(mlp, default):  # noq
     for y in ys:
         R.check("y", y, ry, by)
     assert held.shape == a.shape
+
+
+def test_layers_that_share_a_workspace(mlp):  # noqa: F811
+    """Layers of other shapes and types, one after the other on one workspace: the arrival
+    counts that one leaves zero are not where another keeps its sums."""
+    jobs, need = [], 0
+    shapes = [("bf16", 4, 4096, 384), ("f32", 6, 2048, 520), ("f16", 300, 264, 1001), ("bf16", 64, 1032, 7), ("f32", 700, 96, 40)]
+    for i, (dtype, rows, d_in, d_out) in enumerate(shapes):
+        g = torch.Generator().manual_seed(i)
+        W, b = _layer(g, d_in, d_out, dtype, True)
+        _, x = _rows(g, rows, d_in, dtype, 0)
+        _, dy = _rows(g, rows, d_out, dtype, 0)
+        need = max(need, mlp.mlp_linear_workspace_bytes(W.dtype, d_in, d_out, rows))
+        jobs.append((W, b, x, dy))
+
+    def call(ctx, x, dy):
+        y, z = mlp.mlp_linear_forward(ctx, x, save_z=True)
+        return (y, z) + mlp.mlp_linear_backward(ctx, x, dy, z=z)
+
+    own = [call(mlp.mlp_linear_init(W, b, "gelu", max_rows=x.shape[0]), x, dy) for W, b, x, dy in jobs]
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    ctxs = [mlp.mlp_linear_init(W, b, "gelu", max_rows=x.shape[0], workspace=work) for W, b, x, _ in jobs]
+    for _ in range(3):
+        got = [call(c, x, dy) for c, (_, _, x, dy) in zip(ctxs, jobs)]
+        torch.cuda.synchronize()
+        for a, w in zip(got, own):
+            assert all(torch.equal(s, t) for s, t in zip(a, w))
