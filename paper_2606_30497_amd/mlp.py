@@ -481,6 +481,7 @@ def mlp_deep_last_kernel_ms(ctx: DeepContext) -> float:
 # --- layers: a dense layer and dropout -------------------------------------------
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+FIRST_ROWS = 1024   # room of a context whose caller names no max_rows
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
@@ -531,7 +532,7 @@ _current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda
 class LinearContext:
     """A dense layer's context bound to caller-owned W, bias and workspace."""
 
-    def __init__(self, handle, W, bias, workspace, activation, max_rows, stream, bound):
+    def __init__(self, handle, W, bias, workspace, activation, max_rows, stream, bound, grows=False):
         self.handle = handle
         self.W, self.bias, self.workspace = W, bias, workspace
         self.d_in, self.d_out = W.shape
@@ -540,6 +541,8 @@ class LinearContext:
         self.stream = stream    # None: each call goes on the current stream
         self.bound = bound      # the stream the library's context is on
         self.last = bound       # the stream of the last call that was not captured
+        self.grows = grows      # whether calls of more than max_rows rows make room
+        self.before = []        # the smaller workspaces before this one
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -551,19 +554,9 @@ def mlp_linear_workspace_bytes(dtype: torch.dtype, d_in: int, d_out: int, max_ro
     return int(load().mlp_linear_workspace_bytes(DTYPES[dtype], d_in, d_out, max_rows))
 
 
-def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_BATCH, workspace=None,
-                    stream=None) -> LinearContext:
-    """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
-    bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS. Calls
-    go on `stream`, or on the current stream at each call where none is given; a caller's
-    workspace is taken to be free there (several layers may share one, if their calls do
-    not overlap: over streams the caller orders those). A HIP graph that holds calls replays them on the
-    context's workspace: keep the context as long as the graph."""
+def _linear_context(W, bias, activation, max_rows, workspace, stream):
+    """(handle, workspace) of a context of the library's on `stream`."""
     lib = load()
-    if W.dim() != 2:
-        raise ValueError("W must be [d_in, d_out]")
-    if W.dtype not in DTYPES:
-        raise TypeError("W must be one of %s" % (tuple(DTYPES),))
     d_in, d_out = W.shape
     wp = _dev(W, "W", dtype=W.dtype)
     bp = _vec(bias, "bias", W.dtype, W.device, d_out)
@@ -571,9 +564,8 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
     if need == 0:
         raise MLPError("mlp_linear_workspace_bytes", -2)
     with torch.cuda.device(W.device):
-        bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
         if workspace is None:
-            workspace = _workspace(need, W.device, bound)
+            workspace = _workspace(need, W.device, stream)
         if workspace.device != W.device:
             raise ValueError("workspace is on %s, not on %s" % (workspace.device, W.device))
         _dev(workspace, "workspace", dtype=torch.uint8, numel=need)
@@ -581,8 +573,44 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=MAX_
         _check("mlp_linear_init",
                lib.mlp_linear_init(ctypes.byref(handle), DTYPES[W.dtype], d_in, d_out,
                                    ACTIVATIONS[activation], max_rows, wp, bp, workspace.data_ptr(),
-                                   workspace.numel(), bound))
-    return LinearContext(handle, W, bias, workspace, activation, max_rows, stream, bound)
+                                   workspace.numel(), stream))
+    return handle, workspace
+
+
+def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=None, workspace=None,
+                    stream=None) -> LinearContext:
+    """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
+    bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS.
+    max_rows: the most rows of a call, which the workspace's size goes by; without it (and
+    without a workspace) there is room for 1,024 rows, and a call of more, unless it is
+    captured, makes room for them. Calls go on `stream`, or on the current stream at each
+    call where none is given; a caller's workspace is taken to be free there (several layers
+    may share one, if their calls do not overlap: over streams the caller orders those). A
+    HIP graph that holds calls replays them on the context's workspace: keep the context as
+    long as the graph."""
+    if W.dim() != 2:
+        raise ValueError("W must be [d_in, d_out]")
+    if W.dtype not in DTYPES:
+        raise TypeError("W must be one of %s" % (tuple(DTYPES),))
+    grows = max_rows is None and workspace is None
+    if max_rows is None:
+        max_rows = FIRST_ROWS if grows else MAX_BATCH
+    bound = torch.cuda.current_stream(W.device).cuda_stream if stream is None else stream
+    handle, workspace = _linear_context(W, bias, activation, max_rows, workspace, bound)
+    return LinearContext(handle, W, bias, workspace, activation, max_rows, stream, bound, grows)
+
+
+def _grow(ctx, rows):
+    """Room for `rows` rows, as a power of two (what the library refuses stays refused). Captured
+    calls replay on the workspaces before, which are kept."""
+    with torch.cuda.device(ctx.device), torch.cuda.stream(_stream(ctx.bound, ctx.device)):
+        if rows > MAX_BATCH or torch.cuda.is_current_stream_capturing():
+            return
+    most = 1 << (rows - 1).bit_length()
+    handle, workspace = _linear_context(ctx.W, ctx.bias, ctx.activation, most, None, ctx.bound)
+    load().mlp_linear_destroy(ctx.handle)
+    ctx.before.append(ctx.workspace)
+    ctx.handle, ctx.workspace, ctx.max_rows = handle, workspace, most
 
 
 def mlp_linear_set_stream(ctx: LinearContext, stream) -> None:
@@ -644,6 +672,8 @@ def mlp_linear_forward(ctx: LinearContext, X, residual=None, p=0.0, rng=None, ou
     yp, ldy = _mat(out, "out", dt, dev, rows, n)
     zp, ldz = _mat(z, "z", dt, dev, rows, n)
     _bind_stream(ctx)
+    if rows > ctx.max_rows and ctx.grows:
+        _grow(ctx, rows)
     _check("mlp_linear_forward", load().mlp_linear_forward(ctx.handle, xp, ldx, rows, rp, ldr, float(p), gp, yp,
                                                            ldy, zp, ldz))
     return out if z is None else (out, z)
@@ -673,6 +703,8 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
         raise ValueError("dW must be [%d, %d], is %s" % (ctx.d_in, n, list(dW.shape)))
     dbp = _vec(db, "db", dt, dev, n)
     _bind_stream(ctx)
+    if rows > ctx.max_rows and ctx.grows:
+        _grow(ctx, rows)
     _check("mlp_linear_backward",
            load().mlp_linear_backward(ctx.handle, xp, ldx, zp, ldz, gyp, lddy, rows, float(p), gp,
                                       dxp, lddx, dwp, dbp))

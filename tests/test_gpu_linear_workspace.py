@@ -95,3 +95,42 @@ def test_layers_that_share_a_workspace(mlp):  # noqa: F811
         torch.cuda.synchronize()
         for a, w in zip(got, own):
             assert all(torch.equal(s, t) for s, t in zip(a, w))
+
+
+def test_without_max_rows(mlp):  # noqa: F811
+    """A context takes memory for the rows it is called with (2^20 rows of this layer: 8 GiB),
+    and calls of any rows work; captured ones replay after the workspace has grown."""
+    g = torch.Generator().manual_seed(3)
+    W, b = _layer(g, 1000, 1001, "bf16", True)
+    _, x = _rows(g, 3000, 1000, "bf16", 0)
+    _, dy = _rows(g, 3000, 1001, "bf16", 0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda.synchronize()
+        taken = torch.cuda.memory_allocated()
+        ctx = mlp.mlp_linear_init(W, b, "silu")
+        assert torch.cuda.memory_allocated() - taken < 64 << 20
+        big = mlp.mlp_linear_init(W, b, "silu", max_rows=3000)
+        small = x[:500].clone()
+        want = mlp.mlp_linear_forward(big, small)
+        out = mlp.mlp_linear_forward(ctx, small)
+        torch.cuda.synchronize()
+        gr, too_many = torch.cuda.CUDAGraph(), torch.empty(3000, 1001, dtype=W.dtype, device="cuda")
+        with torch.cuda.graph(gr, stream=s):
+            mlp.mlp_linear_forward(ctx, small, out=out)
+            with pytest.raises(mlp.MLPError):       # no room, and none is made in a capture
+                mlp.mlp_linear_forward(ctx, x, out=too_many)
+        for rows in (1024, 1025, 3000):
+            z = mlp.mlp_linear_forward(big, x[:rows], save_z=True)
+            assert all(torch.equal(a, c) for a, c in zip(mlp.mlp_linear_forward(ctx, x[:rows], save_z=True), z))
+            for a, c in zip(mlp.mlp_linear_backward(ctx, x[:rows], dy[:rows], z=z[1]),
+                            mlp.mlp_linear_backward(big, x[:rows], dy[:rows], z=z[1])):
+                assert torch.equal(a, c)
+            out.zero_()
+            gr.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+        assert ctx.max_rows == 4096 and len(ctx.before) == 2
+    with pytest.raises(mlp.MLPError):
+        mlp.mlp_linear_forward(big, torch.empty(3001, 1000, dtype=W.dtype, device="cuda"))

@@ -188,3 +188,26 @@ def test_workspaces_of_the_whole_nets(world):
         assert ctx.workspace.recorded == ctx.strategy_workspace.recorded == {8}
         mlp.mlp_set_strategy(ctx, "baseline")
         assert ctx.strategy_workspace.pool == 8
+
+
+def test_a_context_that_grows(world):
+    """On the stream of its calls; what the library refuses is left to it."""
+    made = []
+    world.lib.mlp_linear_init = lambda *a: made.append((a[5], a[-1])) or 0
+    world.lib.mlp_linear_destroy = lambda h: None
+    world.current = 5
+    ctx = mlp.mlp_linear_init(Memory(world, (16, 24)), None, "none")
+    first = ctx.workspace
+    assert ctx.grows and made == [(1024, 5)]
+    world.current = 6
+    mlp._bind_stream(ctx)
+    mlp._grow(ctx, 1025)
+    assert made[1:] == [(2048, 6)] and ctx.workspace.pool == 6 and ctx.max_rows == 2048 and ctx.before == [first]
+    world.capturing = {6}
+    mlp._grow(ctx, 5000)
+    world.capturing = set()
+    mlp._grow(ctx, mlp.MAX_BATCH + 1)
+    assert len(made) == 2
+    mlp._grow(ctx, mlp.MAX_BATCH)
+    assert made[2:] == [(mlp.MAX_BATCH, 6)]
+    assert not _layer(world).grows
