@@ -318,10 +318,17 @@ static hipError_t skinny(SkinnyArgs a, int64_t part_floats, int64_t arrived_word
 
 template <class T, bool OUT, bool LOW = false>
 static hipError_t skinny_rows(const SkinnyArgs &a, int64_t part_floats, int64_t arrived_words, hipStream_t stream) {
-    // 16 rows a workgroup, and W read again for every 16 (from the caches: 24 x 8,192 x
-    // 2,048 in bf16 12.0 us so, 17.5 with 32 rows), but 32 where W is too large for that or
-    // the workgroups are more than enough
-    if (a.M <= 16 || (a.N * a.K * (int64_t)sizeof(T) <= (32 << 20) &&
+    // 16 rows a workgroup, and W read again for every 16, from the caches, but 32 where W has
+    // too many elements for that or the workgroups are more than enough. y of 24 rows, W from
+    // memory, us with 16 rows and with 32, d_in x d_out, bf16: 8,192 x 1,024 14.4 and 23.6,
+    // 8,192 x 2,048 15.1 and 19.0, 8,192 x 4,096 20.5 and 22.4, 8,192 x 5,120 25.6 and 23.4, 8,192 x
+    // 8,192 33 and 31; fp32: 8,192 x 2,048 25 and 28, 8,192 x 4,096 40 and 42, 8,192 x 6,144 74 and
+    // 59. Where W's rows do not start at 16 bytes from half as many on (bf16: 8,191 x 2,050 19.1
+    // and 20.0, 6,143 x 4,098 24.3 and 22.2, 8,191 x 6,145 61 and 38), and for dX from a quarter
+    // (bf16: 8,192 x 1,024 10.7 and 10.6, 8,192 x 2,048 15.7 and 15.1, 8,192 x 4,096 28 and 25;
+    // fp32: 8,192 x 1,024 17.7 and 17.1, 8,192 x 2,048 30 and 28, 6,144 x 4,096 46 and 36).
+    const bool whole = OUT && ((uintptr_t)a.W & 15u) == 0 && a.ldw * (int64_t)sizeof(T) % 16 == 0;
+    if (a.M <= 16 || (a.N * a.K <= (whole ? 1 << 25 : OUT ? 1 << 24 : 1 << 23) &&
                       ceil_div(a.M, 16) * ceil_div(a.N, SKINNY_N) <= 256))
         return skinny<T, OUT, 1, LOW>(a, part_floats, arrived_words, stream);
     return skinny<T, OUT, 2, LOW>(a, part_floats, arrived_words, stream);
