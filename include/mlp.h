@@ -405,9 +405,10 @@ mlp_status mlp_linear_forward(mlp_linear_t ctx, const void *X, int64_t ldx, int6
  *   g = dropout(dY) a'(Z);  dX = g W^T;  dW = X^T g;  dbias = column sums of g.
  * For the two products g is rounded to the call's type where that is bf16 or fp16 (the
  * matrix cores take such operands): the error of dX and dW is then about sqrt(2) times that
- * of their own rounding. Not so for 32 rows or fewer, nor for up to 64 while rows d_in d_out
- * <= 2^28 or a width is below 8 (g comes as two values, down to the type's smallest step;
- * an infinity in X or W then gives NaN or an infinity, as with the parts of fp32 operands).
+ * of their own rounding. Not so for 32 rows or fewer, for d_out below 8, nor for up to 64
+ * rows while rows d_in d_out <= 2^28 or d_in is below 8 (g comes as two values, down to the
+ * type's smallest step; an infinity in X or W then gives NaN or an infinity, as with the
+ * parts of fp32 operands).
  * In fp16 g is kept within the type's range by a power of two, so it is finite where dY is.
  * dbias is summed from the unrounded g.
  *   X      [rows x d_in] as in the forward call (used by dW only; may be NULL without)

@@ -249,13 +249,13 @@ static size_t linear_carve(LinearCtx *c, char *ws) {
     };
     const size_t element = dtype_bytes(c->dtype);
     const int64_t M = c->max_rows, K = c->d_in, N = c->d_out;
-    const int64_t more = element == 2 ? (M < REST_ROWS ? M : REST_ROWS) : 0;
+    const int64_t more = element == 4 ? 0 : M < REST_ROWS || N < SKINNY_WIDTH ? M : REST_ROWS;
     const bool twice = element == 2 && any_narrow(*c);
     c->arrived_words = ARRIVED_WORDS;
     c->arrived = (uint32_t *)take(sizeof(uint32_t) * (size_t)c->arrived_words);
     c->g = take(element * (M + more) * pad8(N));
     const bool tiles = M > TILE_ROWS || any_narrow(*c);
-    c->x = take(tiles ? element * (M + (twice ? more : 0)) * pad8(K) : 0);
+    c->x = take(tiles ? element * (M + (twice && N >= SKINNY_WIDTH ? more : 0)) * pad8(K) : 0);
     c->w = take(tiles ? element * (twice ? 2 * K : K) * pad8(N) : 0);
     c->col = (float *)take(M > 64 ? sizeof(float) * grad_chunks(M, N) * (size_t)N : 0);
     c->part_floats = 0;
@@ -363,21 +363,23 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // The products take g rounded to a 16-bit type, a rounding more than their result's own.
     // Of up to 64 rows, where it would show (an element of g is in every value of a row of
     // dX) and W or latency is the bound, what it left goes along as a second value, behind
-    // the first ones of the row. It costs up to a few us (both gradients in bf16, us with
-    // and without: 64 x 4,096 x 1 16.8 and 16.6, 64 x 1 x 4,096 27.4 and 22.6, 64 x 7 x 1,000 22.0
-    // and 18.6), but for large products of 33 to 64 rows (64 x 4,096 x 4,096 50 and 35), which
-    // do without, as more rows do, whose matrix instructions would be twice as many (456 of
-    // the 530 us of 8,192 x 4,096 x 4,096, for an error of dX and dW of 1.65e-3, their own
-    // rounding's, in place of 2.34e-3).
-    const bool rest = sizeof(T) == 2 && M <= REST_ROWS && !as_is && (few || any_narrow(c));
+    // the first ones of the row; and of fewer than eight outputs, whose second values take
+    // columns of the tiles that are idle (both gradients in bf16, us with and without: 65,536 x
+    // 4,096 x 1 343 and 344, 3,000 x 16,384 x 3 63 and 63). Few rows of fewer than eight inputs
+    // pay a few us (64 x 1 x 4,096 27 and 23, 64 x 7 x 1,000 22 and 19). Large products of 33
+    // to 64 rows do without (64 x 4,096 x 4,096 50 and 35), as more rows do, whose matrix
+    // instructions would be twice as many (456 of the 530 us of 8,192 x 4,096 x 4,096, for an
+    // error of dX and dW of 1.65e-3, their own rounding's, in place of 2.34e-3).
+    const bool fold = sizeof(T) == 2 && !as_is && N < SKINNY_WIDTH;
+    const bool rest = fold || (sizeof(T) == 2 && !as_is && M <= REST_ROWS && (few || any_narrow(c)));
     // g that is dY itself: dY is the operand (of few rows, where 32-bit offsets reach over
     // the depth of a step)
     const bool same = as_is && (!few || b.lddy < (1 << 24));
     // what goes to linear_skinny.hip: dX of few_rows, and dW of 32 rows (us there and on
     // tiles, 4,096 x 4,096: bf16 12.5 and 14.6, fp32 33 and 33) or, for the second values, 64
     const bool outer = few && M <= (sizeof(T) == 4 ? TILE_ROWS : REST_ROWS);
-    // Second values on tiles: (g, low) by (w, w) along the depth of dX, and by x in the row of
-    // g and in that of low for dW, whose rows alternate.
+    // Second values on tiles: (g, low) by (w, w) along the depth of dX; for dW as columns of
+    // their own, which are folded, or by x in the row of g and in that of low, which alternate.
     const bool twice = rest && !few;
     const float scale = std::is_same<T, f16>::value && !as_is ? headroom(c.act, b.drop) : 1.0f;
     const int64_t low = rest ? pad8(N) : 0, ldg = pad8(N) + low;
@@ -390,7 +392,7 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     // (16-bit rows that start at odd elements load slowly: where many rows of g read W, it is
     // laid out first for k_skinny too: 700 x 30 x 10,001 in bf16 29 us, 20 so)
     if (b.dX && M > 0 && (!few || (sizeof(T) == 2 && M > 128 && N % 2))) w = o.get<T>(c.W, N, K, N, c.w, twice);
-    if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x, twice);
+    if (b.dW && !outer) x = o.get<T>(b.X, b.ldx, M, K, c.x, twice && !fold);
     if (hipError_t e = o.launch<T>()) return e;
     int64_t chunks = 0;
     if (M > 0 && (b.db || (products && !same))) {
@@ -438,6 +440,8 @@ static hipError_t linear_backward(const LinearCtx &c, const BackwardArgs &b) {
     if (outer) return launch_outer(c.dtype, b.X, b.ldx, g.p, g.ld, low, M, K, N, scale, b.dW, c.stream);
     e.Y = b.dW;
     e.ldy = N;
+    if (fold)
+        return launch_gemm_fold(c.dtype, x, g, K, N, M, e, c.part, c.part_floats, c.stream);
     if (twice) g.ld = g.len = low;
     return launch_gemm(GEMM_TN, c.dtype, x, g, K, N, twice ? 2 * M : M, e, c.part, c.part_floats, c.stream);
 }

@@ -155,8 +155,9 @@ __device__ __forceinline__ void chunk_step(const TA &a, const TB &b, f16v (&acc)
 }
 
 // TM x TN outputs, WM x WN waves, each TM / WM x TN / WN outputs as 32 x 32 MFMA tiles. T: the
-// type of C. S: LDS stages, each a chunk of both operands.
-template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN>
+// type of C. S: LDS stages, each a chunk of both operands. FOLD: fewer than eight columns,
+// B's rows hold two values of each, eight apart.
+template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN, bool FOLD>
 __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
     constexpr int NT = 64 * WM * WN, MI = TM / WM / 32, NJ = TN / WN / 32;
     typedef Tile<OP == GEMM_TN, TM, BK, NT> TA;
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
         TA a;
         TB b;
         a.init(g.A, at.m0, g.M, at.kb);
-        b.init(g.B, at.n0, g.N, at.kb);
+        b.init(g.B, at.n0, FOLD ? 16 : g.N, at.kb);
         // S - 1 chunks are on their way before the first is used. At chunk c's barrier
         // every wave has loaded chunks c and c + 1 and read all of chunk c - 1, whose
         // stage chunk c + S - 1 takes. (Past the last chunk zeros are loaded, so that the
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_tile(const GemmArgs g) {
         loaded_all_but<0>();   // no load to LDS is under way when the results take its place
     }
 
-    finish_tile<T>(g, at, wm, wn, acc, reinterpret_cast<float *>(lds));
+    finish_tile<T, FOLD>(g, at, wm, wn, acc, reinterpret_cast<float *>(lds));
 }
 
 // The splits' sums, in order, through the epilogue.
@@ -267,12 +268,12 @@ hipError_t join_splits(const GemmArgs &g, hipStream_t stream) {
 }
 template hipError_t join_splits<float>(const GemmArgs &, hipStream_t);
 
-template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN>
+template <class T, int OP, int TM, int TN, int BK, int S, int WM, int WN, bool FOLD = false>
 static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream) {
     // (a chunk of 64 takes 0.28 us on 64 x 64 tiles, 0.5 on 128 x 128, 1 and more on 256 x 256)
     constexpr int WORTH = (TM == 64 ? 1024 : TM == 128 ? 576 : 256) / BK;
     const unsigned grid = plan_tiles(g, TM, TN, BK, CUS, WORTH, part_floats);
-    hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, S, WM, WN>), dim3(grid), dim3(64 * WM * WN), 0, stream, g);
+    hipLaunchKernelGGL((k_gemm_tile<T, OP, TM, TN, BK, S, WM, WN, FOLD>), dim3(grid), dim3(64 * WM * WN), 0, stream, g);
     if (hipError_t e = hipGetLastError()) return e;
     return join_splits<T>(g, stream);
 }
@@ -287,17 +288,18 @@ static hipError_t gemm_tiles(GemmArgs g, int64_t part_floats, hipStream_t stream
 // 128 x 128 of four stages where no split is needed (1,536 x 1,536 x 1,536 18, on 64 x 64 22),
 // or the depth pays for the splits' joining (1,024 x 1,024 x 16,384 58 and 76, of 1,024 23 and
 // 8.6; TN, whose 64 x 64 tiles are slower, of 4,096 27 and 36, of 2,048 22 and 14).
-template <class T, int OP>
+template <class T, int OP, bool FOLD = false>
 static hipError_t gemm_op(const GemmArgs &g, int64_t part_floats, hipStream_t stream) {
     constexpr bool TN = OP == GEMM_TN;
     const int64_t big = ceil_div(g.M, 256) * ceil_div(g.N, 256), mid = ceil_div(g.M, 128) * ceil_div(g.N, 128);
-    if (big > CUS / 2 && 16 * big <= 5 * mid)
-        return gemm_tiles<T, OP, 256, 256, TN ? 32 : 64, TN ? 5 : 2, 2, 4>(g, part_floats, stream);
+    if constexpr (!FOLD)   // (a column of tiles never covers so little)
+        if (big > CUS / 2 && 16 * big <= 5 * mid)
+            return gemm_tiles<T, OP, 256, 256, TN ? 32 : 64, TN ? 5 : 2, 2, 4>(g, part_floats, stream);
     if constexpr (!TN)
         if (mid > CUS) return gemm_tiles<T, OP, 128, 128, 64, 2, 2, 2>(g, part_floats, stream);
     if (mid > CUS / 2 || (mid >= 16 && g.K > (TN ? 2048 : 4096)))
-        return gemm_tiles<T, OP, 128, 128, TN ? 32 : 64, 4, 2, TN ? 2 : 4>(g, part_floats, stream);
-    return gemm_tiles<T, OP, 64, 64, 64, 4, 2, 2>(g, part_floats, stream);
+        return gemm_tiles<T, OP, 128, 128, TN ? 32 : 64, 4, 2, TN ? 2 : 4, FOLD>(g, part_floats, stream);
+    return gemm_tiles<T, OP, 64, 64, 64, 4, 2, 2, FOLD>(g, part_floats, stream);
 }
 
 template <class T>
@@ -307,6 +309,20 @@ static hipError_t gemm_type(int op, const GemmArgs &g, int64_t part_floats, hipS
     case GEMM_NT: return gemm_op<T, GEMM_NT>(g, part_floats, stream);
     default: return gemm_op<T, GEMM_TN>(g, part_floats, stream);
     }
+}
+
+hipError_t launch_gemm_fold(int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N, int64_t K,
+                            const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream) {
+    GemmArgs g{};
+    g.A = A;
+    g.B = B;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.part = part;
+    g.e = e;
+    if (dtype == MLP_BF16) return gemm_op<bf16, GEMM_TN, true>(g, part_floats, stream);
+    return gemm_op<f16, GEMM_TN, true>(g, part_floats, stream);
 }
 
 hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N,

@@ -82,6 +82,11 @@ struct GemmArgs {
 hipError_t launch_gemm(int op, int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N,
                        int64_t K, const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream);
 
+// The 16-bit GEMM_TN of N < 8 outputs where B counts as the sum of two: its rows are of 16
+// elements, the second values from the eighth on.
+hipError_t launch_gemm_fold(int32_t dtype, const Operand &A, const Operand &B, int64_t M, int64_t N, int64_t K,
+                            const Epilogue &e, float *part, int64_t part_floats, hipStream_t stream);
+
 hipError_t launch_gemm_f32(int op, const GemmArgs &g, int64_t part_floats, hipStream_t stream);
 // the splits' sums through the epilogue, where there are splits
 template <class T>

@@ -93,11 +93,12 @@ struct TileAt {
 // on, the columns the first operand), 32 rows at a time, through LDS (lds: 32 rows of
 // RESULT_STRIDE floats for each wave): a lane's registers hold four columns here and there
 // of one row, memory is read and written along the rows. A lane's columns are the same in
-// all rows; the residual's rows are read ahead.
+// all rows; the residual's rows are read ahead. FOLD: columns 8 to 15 are added to the first eight,
+// which are all there are.
 template <int NJ>
 constexpr int RESULT_STRIDE = 32 * NJ + 4;
 
-template <class T, int NJ, int MI>
+template <class T, bool FOLD = false, int NJ, int MI>
 __device__ __forceinline__ void finish_tile(const GemmArgs &g, const TileAt &at, int wm, int wn,
                                             const f16v (&acc)[NJ][MI], float *lds) {
     constexpr int WTN = 32 * NJ, CS = RESULT_STRIDE<NJ>;
@@ -141,6 +142,10 @@ __device__ __forceinline__ void finish_tile(const GemmArgs &g, const TileAt &at,
             const f4 *c = reinterpret_cast<const f4 *>(C + (lr + k * ROWS) * CS + 8 * (lane % GROUPS));
 #pragma unroll
             for (int x = 0; x < 8; ++x) v[x] = c[x / 4][x % 4];
+            if constexpr (FOLD) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] += c[2 + x / 4][x % 4];
+            }
             if (!whole) store8(g.part + ((int64_t)at.split * g.M + r) * g.N, n, g.N, v);
             else fin.finish(g.e, r, n, g.N, v, res[k]);
         }

@@ -1,6 +1,6 @@
 """Gradients of up to 64 rows in bf16 and fp16 take g = dropout(dY) a'(Z) unrounded, as two
-values of the type (large products of 33 and more rows apart): held to a bound without the
-rounding of g, at any widths.
+values of the type (large products of 33 and more rows apart), at any widths, and so do those
+of fewer than eight outputs at any rows: held to a bound without the rounding of g.
 
 The bound, with u half a step of the type, e = 2^-24 and t half the type's smallest step:
 - the two values leave at most u^2 |g| + t of an element of g (the second one's rounding);
@@ -106,3 +106,21 @@ def test_gradients_of_up_to_64_rows(mlp, dtype, rows, d_in, d_out):
         z = None if act == "none" else far[1]
         assert torch.equal(mlp.mlp_linear_backward(ctx, None, far[2], z=z, p=p, rng=rng, need_dw=False)[0], dx)
         assert torch.equal(mlp.mlp_linear_backward(ctx, far[0], far[2], z=z, p=p, rng=rng, need_dx=False)[1], dw)
+
+
+# 64 x 64 tiles, split and not, and 128 x 128 ones, by their number and for a deep product
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,d_in,d_out", [(65, 24, 1), (333, 777, 2), (1000, 64, 3), (3001, 40, 4), (700, 130, 5),
+                                             (9000, 21, 6), (2100, 264, 7), (600, 1, 1), (130, 16500, 3), (3000, 2100, 5)])
+def test_gradients_of_fewer_than_eight_outputs(mlp, dtype, rows, d_in, d_out):
+    print(dtype, rows, d_in, d_out, flush=True)
+    X, W, Z, dY = (t.cuda() for t in inputs(rows, d_in, d_out, dtype, rows))
+    rng = torch.tensor([6, 7], device="cuda")
+    ctx = mlp.mlp_linear_init(W, None, "gelu", max_rows=rows)
+    dx, dw, _ = mlp.mlp_linear_backward(ctx, X, dY, z=Z, p=0.2, rng=rng)
+    torch.cuda.synchronize()
+    ref, _ = gradients(X, W, Z, dY, "gelu", 0.2, (6, 7), dtype)
+    R.check("dx", dx, *ref["dx"])
+    R.check("dw", dw, *ref["dw"])
+    assert torch.equal(mlp.mlp_linear_backward(ctx, X, dY, z=Z, p=0.2, rng=rng, need_dx=False)[1], dw)
