@@ -581,9 +581,9 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=None
                     stream=None) -> LinearContext:
     """A dense layer y = residual + dropout(a(X W + bias)). W [d_in, d_out] (float32,
     bfloat16 or float16), bias [d_out] or None; activation a name of ACTIVATIONS.
-    max_rows: the most rows of a call, which the workspace's size goes by; without it (and
-    without a workspace) there is room for 1,024 rows, and a call of more, unless it is
-    captured, makes room for them. Calls go on `stream`, or on the current stream at each
+    max_rows: the most rows of a call, which the workspace's size goes by; without it there is
+    room for 1,024 rows, and a call of more, unless it is captured, makes room for them (with a
+    workspace of the caller's it is the most there may be, 2^20). Calls go on `stream`, or on the current stream at each
     call where none is given; a caller's workspace is taken to be free there (several layers
     may share one, if their calls do not overlap: over streams the caller orders those). A
     HIP graph that holds calls replays them on the context's workspace: keep the context as
@@ -592,6 +592,7 @@ def mlp_linear_init(W: torch.Tensor, bias=None, activation="none", max_rows=None
         raise ValueError("W must be [d_in, d_out]")
     if W.dtype not in DTYPES:
         raise TypeError("W must be one of %s" % (tuple(DTYPES),))
+    _dev(W, "W", dtype=W.dtype)
     grows = max_rows is None and workspace is None
     if max_rows is None:
         max_rows = FIRST_ROWS if grows else MAX_BATCH
