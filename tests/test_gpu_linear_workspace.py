@@ -134,3 +134,38 @@ def test_without_max_rows(mlp):  # noqa: F811
         assert ctx.max_rows == 4096 and len(ctx.before) == 2
     with pytest.raises(mlp.MLPError):
         mlp.mlp_linear_forward(big, torch.empty(3001, 1000, dtype=W.dtype, device="cuda"))
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_captured_on_a_stream_of_the_graphs_own(mlp, rows):  # noqa: F811
+    """Eager calls on one stream, a capture on the stream that torch makes for it, replays with
+    eager calls of other rows in between, the context dropped after the last."""
+    g = torch.Generator().manual_seed(rows)
+    W, b = _layer(g, 2048, 264, "bf16", True)
+    _, x = _rows(g, rows, 2048, "bf16", 0)
+    _, dy = _rows(g, rows, 264, "bf16", 0)
+    ctx = mlp.mlp_linear_init(W, b, "gelu")
+
+    def call(k):
+        y, z = mlp.mlp_linear_forward(ctx, x[:k], save_z=True)
+        return (y, z) + mlp.mlp_linear_backward(ctx, x[:k], dy[:k], z=z)
+
+    call(rows)
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        held = call(rows)
+    side = torch.cuda.Stream()
+    for k in range(4):
+        gr.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in held]
+        with torch.cuda.stream(side):
+            call(rows - 1)
+        eager = call(rows)
+        torch.cuda.synchronize()
+        assert all(torch.equal(s, t) for s, t in zip(replayed, eager))
+        x.mul_(-0.5)
+        torch.cuda.synchronize()
+    gr.reset()
+    del ctx
+    torch.cuda.synchronize()
