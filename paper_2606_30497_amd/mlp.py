@@ -692,6 +692,8 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
     gyp, lddy = _mat(dY, "dY", dt, dev, rows, n)
     zp, ldz = _mat(z, "z", dt, dev, rows, n)
     gp = _rng(rng, dev)
+    if dW is not None and dW.dim() != 1 and dW.shape != (ctx.d_in, n):   # (flat: a slice of a bucket)
+        raise ValueError("dW must be [%d, %d], is %s" % (ctx.d_in, n, list(dW.shape)))
     if dX is None and need_dx:
         dX = _new(ctx, rows, ctx.d_in)
     if dW is None and need_dw:
@@ -700,8 +702,6 @@ def mlp_linear_backward(ctx: LinearContext, X, dY, z=None, p=0.0, rng=None, need
         db = _new(ctx, n)
     dxp, lddx = _mat(dX, "dX", dt, dev, rows, ctx.d_in)
     dwp = _vec(dW, "dW", dt, dev, ctx.d_in * n)
-    if dW is not None and dW.dim() != 1 and dW.shape != (ctx.d_in, n):   # (flat: a slice of a bucket)
-        raise ValueError("dW must be [%d, %d], is %s" % (ctx.d_in, n, list(dW.shape)))
     dbp = _vec(db, "db", dt, dev, n)
     _bind_stream(ctx)
     if rows > ctx.max_rows and ctx.grows:
